@@ -22,9 +22,9 @@ def _forward(name, dtype, n, k, m, act="identity", bias=False, residual=False, s
     return dict(c, name=name) if name else c
 
 
-def _backward(name, dtype, n, k, m, act="identity", scale=1.0, x_cols=False, w_cols=False, gx=True, gw=True, gbias=True, grads="same"):
+def _backward(name, dtype, n, k, m, act="identity", scale=1.0, x_cols=False, w_cols=False, gx=True, gw=True, gbias=True):
     c = dict(op="backward", dtype=dtype, n=n, k=k, m=m, act=act, scale=scale, x_cols=x_cols, w_cols=w_cols, gx=gx, gw=gw,
-             gbias=gbias, grads=grads)
+             gbias=gbias)
     return dict(c, name=name) if name else c
 
 
@@ -51,8 +51,8 @@ def listed():
         _forward("forward_large", "bf16", 8_192, 8_192, 8_192, act="gelu_tanh", bias=True, residual=True),
         # minus the gradient of a squared loss: X^T resid on the smallest dense configuration
         _backward("gradient_small", "f32", 1_000, 10_000, 1, scale=-1.0, x_cols=True, gx=False, gbias=False),
-        # sizes that divide by nothing, gradients of the weights kept in 32 bits
-        _backward("backward_ragged", "f16", 333, 1_001, 517, act="silu", grads="f32"),
+        # sizes that divide by nothing
+        _backward("backward_ragged", "f16", 333, 1_001, 517, act="silu"),
         # a training batch back through a layer
         _backward("backward_large", "bf16", 4_096, 4_096, 8_192, act="gelu"),
         # the coefficients and intercepts of a few small models, with the L1 threshold
@@ -86,7 +86,7 @@ def draw(rng):
     shape = dict(act=rng.choice(ACTS), scale=rng.choice((1.0, -1.0, 0.5)), x_cols=rng.random() < 0.3, w_cols=rng.random() < 0.3)
     if op == "forward":
         return _forward(None, dtype, n, k, m, bias=rng.random() < 0.7, residual=rng.random() < 0.5, preact=rng.random() < 0.3, **shape)
-    return _backward(None, dtype, n, k, m, gx=rng.random() < 0.8, gbias=rng.random() < 0.7, grads=rng.choice(("same", "f32")), **shape)
+    return _backward(None, dtype, n, k, m, gx=rng.random() < 0.8, gbias=rng.random() < 0.7, **shape)
 
 
 # ---- inputs ----
@@ -136,43 +136,46 @@ def _cut(case, flat):
     return [flat[a:a + n] for a, n in zip(_starts(case)[0], _sizes(case))]
 
 
+def _blocks(case):
+    """Where the elements of each block of 256 lie in the flat buffer, [blocks, 256], and which of them there are: a tensor's
+    last block may be shorter, and no block spans two tensors.  Also the number of blocks of each tensor."""
+    length = torch.tensor(_sizes(case), device="cuda")
+    count = (length + BLOCK - 1) // BLOCK
+    tensor = torch.arange(len(length), device="cuda").repeat_interleave(count)
+    inside = torch.arange(len(tensor), device="cuda") - (count.cumsum(0) - count)[tensor]
+    at = inside[:, None] * BLOCK + torch.arange(BLOCK, device="cuda")
+    there = at < length[tensor][:, None]
+    return torch.where(there, at + torch.tensor(_starts(case)[0], device="cuda")[tensor][:, None], 0), there, count.tolist()
+
+
 def _encode_m(m):
-    n = m.numel()
-    rows = torch.nn.functional.pad(m, (0, -n % BLOCK)).view(-1, BLOCK)
-    mag = rows.abs()
-    top = torch.where(torch.isfinite(mag), mag, torch.zeros_like(mag)).amax(1)
-    s = torch.where(top >= 2.0 ** -100, top / 16129.0, torch.zeros_like(top))
-    r = torch.where(s > 0, 1.0 / s, torch.zeros_like(s))
+    """Codes and scales of first moments in blocks [blocks, 256]: m = s q |q|, q = -128 where it is not finite."""
+    mag = m.abs()
+    top = torch.where(torch.isfinite(mag), mag, 0.0).amax(1)
+    s = torch.where(top >= 2.0 ** -100, top / 16129.0, 0.0)
+    r = torch.where(s > 0, 1.0 / s, 0.0)
     q = torch.round(torch.sqrt(mag * r[:, None]))
-    q = torch.where(torch.isfinite(mag), torch.where(rows < 0, -q, q), torch.full_like(q, -128.0))
-    return q.view(-1)[:n].to(torch.int8), s
+    return torch.where(torch.isfinite(mag), torch.where(m < 0, -q, q), -128.0).to(torch.int8), s
 
 
 def _encode_root(root):
-    n = root.numel()
-    rows = torch.nn.functional.pad(root, (0, -n % BLOCK)).view(-1, BLOCK)
-    top = torch.where(torch.isfinite(rows), rows, torch.zeros_like(rows)).amax(1)
-    s = torch.where(top >= 2.0 ** -100, top / 64516.0, torch.zeros_like(top))
-    r = torch.where(s > 0, 1.0 / s, torch.zeros_like(s))
-    q = torch.round(torch.sqrt(rows * r[:, None]))
-    q = torch.where(rows > 0, q.clamp(min=1.0), q)
-    q = torch.where(torch.isfinite(rows), q, torch.full_like(q, 255.0))
-    return q.view(-1)[:n].to(torch.uint8), s
-
-
-def _spread(s, n):
-    return s.repeat_interleave(BLOCK)[:n]
+    """Codes and scales of the roots of second moments: sqrt(v) = s q^2, q = 255 where it is not finite, at least 1 where it is not 0."""
+    top = torch.where(torch.isfinite(root), root, 0.0).amax(1)
+    s = torch.where(top >= 2.0 ** -100, top / 64516.0, 0.0)
+    r = torch.where(s > 0, 1.0 / s, 0.0)
+    q = torch.round(torch.sqrt(root * r[:, None]))
+    q = torch.where(root > 0, q.clamp(min=1.0), q)
+    return torch.where(torch.isfinite(root), q, 255.0).to(torch.uint8), s
 
 
 def _decode_m(q, s):
     v = q.float()
-    return torch.where(q == -128, torch.full_like(v, float("nan")), (v * v.abs()) * _spread(s, q.numel()))
+    return torch.where(q == -128, float("nan"), (v * v.abs()) * s[:, None])
 
 
-def _decode_v(q, s):
+def _decode_root(q, s):
     v = q.float()
-    root = (v * v) * _spread(s, q.numel())
-    return torch.where(q == 255, torch.full_like(v, float("nan")), root * root)
+    return torch.where(q == 255, float("nan"), (v * v) * s[:, None])
 
 
 def _adamw_inputs(case, seed):
@@ -187,14 +190,16 @@ def _adamw_inputs(case, seed):
     g = normal().mul_(size).div_(case["grad_scale"])
     m = normal().mul_(size).mul_(0.3)
     v = torch.rand(total, generator=gen, device="cuda").add_(0.05).mul_(size).mul_(size)
-    d = dict(params=p.to(DTYPES[case["params"]]), grads=g.to(DTYPES[case["grads"]]), masters=p if case["masters"] else None)
-    if case["bits"] == 32:
-        d["first"], d["second"] = m, v
-        d["moments"] = (_cut(case, m), _cut(case, v))
-    else:
-        first = [_encode_m(t) for t in _cut(case, m)]
-        second = [_encode_root(t.sqrt()) for t in _cut(case, v)]
-        d["moments"] = ([q for q, _ in first], [s for _, s in first], [q for q, _ in second], [s for _, s in second])
+    d = dict(params=p.to(DTYPES[case["params"]]), grads=g.to(DTYPES[case["grads"]]))
+    if case["masters"]:
+        d["masters"] = p
+    d["first"], d["second"] = m, v
+    if case["bits"] == 8:
+        at, there, _ = _blocks(case)
+        rows = lambda t: torch.where(there, t[at], 0.0)
+        (q1, d["scale1"]), (q2, d["scale2"]) = _encode_m(rows(m)), _encode_root(rows(v).sqrt())
+        d["code1"] = torch.zeros(total, dtype=torch.int8, device="cuda").index_put_((at[there],), q1[there])
+        d["code2"] = torch.zeros(total, dtype=torch.uint8, device="cuda").index_put_((at[there],), q2[there])
         d["first"], d["second"] = torch.zeros_like(m), torch.zeros_like(v)      # where the values go that the codes stand for
     return d
 
@@ -206,12 +211,21 @@ def prepare(case, seed):
     if case["op"] != "adamw":
         return dict(case=case, **_layer_inputs(case, seed))
     state = dict(case=case, step=case["step"], **_adamw_inputs(case, seed))
-    masters = _cut(case, state["masters"]) if case["masters"] else None
-    state["lists"] = dict(params=_cut(case, state["params"]), grads=_cut(case, state["grads"]), masters=masters,
-                          first=_cut(case, state["first"]), second=_cut(case, state["second"]))
+    # the tensors of the network: views of the flat buffers
+    lists = {key: _cut(case, t) for key, t in state.items() if isinstance(t, torch.Tensor) and not key.startswith("scale")}
+    if case["bits"] == 8:
+        state["at"], state["there"], count = _blocks(case)
+        moments = (lists["code1"], state["scale1"].split(count), lists["code2"], state["scale2"].split(count))
+    else:
+        inside = torch.zeros(state["params"].numel(), dtype=torch.bool, device="cuda")
+        for t in _cut(case, inside):
+            t.fill_(True)
+        state["inside"] = inside
+        moments = (lists["first"], lists["second"])
+    state["lists"] = lists
     if own:
         from paper_1312_5766_b200 import binding
-        state["opt"] = binding.AdamW(state["lists"]["params"], bits=case["bits"], masters=masters, moments=state["moments"],
+        state["opt"] = binding.AdamW(lists["params"], bits=case["bits"], masters=lists.get("masters"), moments=moments,
                                      betas=(BETA1, BETA2), eps=EPS, weight_decay=case["weight_decay"], l1=case["l1"])
     return state
 
@@ -264,7 +278,6 @@ def _plain_forward(st):
 def _plain_backward(st):
     c = st["case"]
     dt = st["x"].dtype
-    gdt = dt if c["grads"] == "same" else torch.float32
     gz = c["scale"] * st["gout"].float()
     if c["act"] != "identity":
         gz = gz * _act_slope(st["preact"].float(), c["act"])
@@ -272,9 +285,9 @@ def _plain_backward(st):
     if c["gx"]:
         out.append((gz @ st["w"].float()).to(dt))
     if c["gw"]:
-        out.append((gz.t() @ st["x"].float()).to(gdt))
+        out.append((gz.t() @ st["x"].float()).to(dt))
     if c["gbias"]:
-        out.append(gz.sum(0).to(gdt))
+        out.append(gz.sum(0).to(dt))
     return out
 
 
@@ -284,33 +297,42 @@ def _plain_adamw(st):
     b1, ob1, b2, ob2 = f32(BETA1), f32(1.0 - BETA1), f32(BETA2), f32(1.0 - BETA2)
     move, unbias, keep = f32(LR / (1.0 - BETA1 ** t)), f32(1.0 / math.sqrt(1.0 - BETA2 ** t)), f32(1.0 - LR * c["weight_decay"])
     threshold = f32(LR * c["l1"])
-    lists = st["lists"]
-    for i, p in enumerate(lists["params"]):
-        g = lists["grads"][i].float() * c["grad_scale"]
-        if c["bits"] == 32:
-            m, v = lists["first"][i], lists["second"][i]
-        else:
-            m = _decode_m(st["moments"][0][i], st["moments"][1][i])
-            v = _decode_v(st["moments"][2][i], st["moments"][3][i])
-        m = m * b1 + g * ob1
-        v = v * b2 + (g * g) * ob2
-        root = torch.sqrt(v)
-        inv = 1.0 / (root * unbias + EPS)
-        at = lists["masters"][i] if c["masters"] else p.float()
-        at = at * keep - (m * move) * inv
-        if c["l1"] > 0:
-            size = (at.abs() - threshold * inv).clamp(min=0.0)
-            at = torch.where(at < 0, -size, size)
-        p.copy_(at)
-        if c["masters"]:
-            lists["masters"][i].copy_(at)
-        if c["bits"] == 8:
-            for j, codes in enumerate(_encode_m(m) + _encode_root(root)):
-                st["moments"][j][i].copy_(codes)
-            m = _decode_m(st["moments"][0][i], st["moments"][1][i])
-            v = _decode_v(st["moments"][2][i], st["moments"][3][i])
-        lists["first"][i].copy_(m)
-        lists["second"][i].copy_(v)
+    at = st["masters"] if c["masters"] else st["params"].float()
+    g = st["grads"].float() * c["grad_scale"]
+    if c["bits"] == 32:
+        m, v = st["first"], st["second"]
+    else:
+        where, there = st["at"], st["there"]
+        rows = lambda t: torch.where(there, t[where], 0)
+        at, g = rows(at), rows(g)
+        m = _decode_m(rows(st["code1"]), st["scale1"])
+        root = _decode_root(rows(st["code2"]), st["scale2"])
+        v = root * root
+    m = m * b1 + g * ob1
+    v = v * b2 + (g * g) * ob2
+    root = torch.sqrt(v)
+    inv = 1.0 / (root * unbias + EPS)
+    at = at * keep - (m * move) * inv
+    if c["l1"] > 0:
+        size = (at.abs() - threshold * inv).clamp(min=0.0)
+        at = torch.where(at < 0, -size, size)
+    if c["bits"] == 32:
+        put = lambda flat, t: flat.copy_(torch.where(st["inside"], t.to(flat.dtype), flat))
+    else:
+        where = where[there]
+        put = lambda flat, t: flat.index_put_((where,), t[there].to(flat.dtype))
+        (q1, s1), (q2, s2) = _encode_m(m), _encode_root(root)
+        st["scale1"].copy_(s1)
+        st["scale2"].copy_(s2)
+        put(st["code1"], q1)
+        put(st["code2"], q2)
+        m, root = _decode_m(q1, s1), _decode_root(q2, s2)
+        v = root * root
+    put(st["params"], at)
+    if c["masters"]:
+        put(st["masters"], at)
+    put(st["first"], m)
+    put(st["second"], v)
     return _adamw_outputs(st)
 
 
@@ -332,8 +354,7 @@ def run(state):
             return _plain_backward(state)
         from paper_1312_5766_b200 import binding
         grads = binding.linear_backward(state["gout"], state["x"], state["w"], preact=state["preact"], activation=c["act"],
-                                        scale=c["scale"], want_x=c["gx"], want_w=c["gw"], want_bias=c["gbias"],
-                                        grad_dtype=torch.float32 if c["grads"] == "f32" else None)
+                                        scale=c["scale"], want_x=c["gx"], want_w=c["gw"], want_bias=c["gbias"])
         return [g for g in grads if g is not None]
     if not own:
         out = _plain_adamw(state)
@@ -357,9 +378,8 @@ def work(case):
     if case["op"] == "forward":
         out = n * m * s
         return {"bytes": s * (n * k + m * k + (m if case["bias"] else 0)) + out * (1 + case["residual"] + case["preact"]), "flops": 2 * n * k * m}
-    gs = s if case["grads"] == "same" else 4
     b = s * n * m * (2 if case["act"] != "identity" else 1)
-    b += (s * (m * k + n * k) if case["gx"] else 0) + (s * n * k + gs * m * k if case["gw"] else 0) + (gs * m if case["gbias"] else 0)
+    b += (s * (m * k + n * k) if case["gx"] else 0) + (s * (n * k + m * k) if case["gw"] else 0) + (s * m if case["gbias"] else 0)
     return {"bytes": b, "flops": 2 * n * k * m * (case["gx"] + case["gw"])}
 
 
@@ -411,27 +431,23 @@ def exact(case, seed):
 
 def _exact_adamw(case, seed):
     d = _adamw_inputs(case, seed)
-    t, grads, starts = case["step"], _cut(case, d["grads"]), _starts(case)[0]
-    flat = lambda key: d[key].double()
-    at_all, first, second = flat("masters" if case["masters"] else "params"), flat("first"), flat("second")
-    params = flat("params")                                      # (what lies between two tensors stays as it is)
-    for i, n in enumerate(_sizes(case)):
-        here = slice(starts[i], starts[i] + n)
-        g = grads[i].double() * case["grad_scale"]
-        if case["bits"] == 32:
-            m, v = first[here], second[here]
-        else:
-            block = torch.arange(n, device="cuda") // BLOCK
-            q = d["moments"][0][i].double()
-            m = q.sign() * q ** 2 * d["moments"][1][i].double()[block]
-            v = d["moments"][2][i].double() ** 4 * d["moments"][3][i].double()[block] ** 2
-        m = BETA1 * m + (1 - BETA1) * g
-        v = BETA2 * v + (1 - BETA2) * g ** 2
-        metric = (v / (1 - BETA2 ** t)).sqrt() + EPS
-        at = at_all[here] * (1 - LR * case["weight_decay"]) - LR * m / (1 - BETA1 ** t) / metric
-        if case["l1"] > 0:
-            at = torch.sgn(at) * (at.abs() - LR * case["l1"] / metric).clamp(min=0)
-        at_all[here], params[here], first[here], second[here] = at, at, m, v
-    if case["bits"] == 8:
-        first = second = None      # a moment held in 8 bits is the nearest code of its block, not the number itself
-    return [params, first, second] + ([at_all] if case["masters"] else [])
+    t, at, there = case["step"], *_blocks(case)[:2]
+    at = at[there]                                                # (what lies between two tensors stays as it is)
+    if case["bits"] == 32:
+        m, v = d["first"].double()[at], d["second"].double()[at]
+    else:
+        q = d["code1"][at].double()
+        m = q.sign() * q ** 2 * d["scale1"].double()[:, None].expand(there.shape)[there]
+        v = (d["code2"][at].double() ** 2 * d["scale2"].double()[:, None].expand(there.shape)[there]) ** 2
+    g = d["grads"].double()[at] * case["grad_scale"]
+    m = BETA1 * m + (1 - BETA1) * g
+    v = BETA2 * v + (1 - BETA2) * g ** 2
+    metric = (v / (1 - BETA2 ** t)).sqrt() + EPS
+    p = d["masters" if case["masters"] else "params"].double()[at]
+    p = p * (1 - LR * case["weight_decay"]) - LR * m / (1 - BETA1 ** t) / metric
+    if case["l1"] > 0:
+        p = torch.sgn(p) * (p.abs() - LR * case["l1"] / metric).clamp(min=0)
+    put = lambda key, new: d[key].double().index_put_((at,), new)
+    # a moment held in 8 bits is the nearest code of its block, not the number itself
+    moments = [put("first", m), put("second", v)] if case["bits"] == 32 else [None, None]
+    return [put("params", p)] + moments + ([put("masters", p)] if case["masters"] else [])
