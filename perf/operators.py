@@ -152,7 +152,7 @@ def _encode_m(m):
     """Codes and scales of first moments in blocks [blocks, 256]: m = s q |q|, q = -128 where it is not finite."""
     mag = m.abs()
     top = torch.where(torch.isfinite(mag), mag, 0.0).amax(1)
-    s = torch.where(top >= 2.0 ** -100, top / 16129.0, 0.0)
+    s = torch.where(top >= 2.0 ** -100, top * (1.0 / 16129.0), 0.0)
     r = torch.where(s > 0, 1.0 / s, 0.0)
     q = torch.round(torch.sqrt(mag * r[:, None]))
     return torch.where(torch.isfinite(mag), torch.where(m < 0, -q, q), -128.0).to(torch.int8), s
@@ -161,7 +161,7 @@ def _encode_m(m):
 def _encode_root(root):
     """Codes and scales of the roots of second moments: sqrt(v) = s q^2, q = 255 where it is not finite, at least 1 where it is not 0."""
     top = torch.where(torch.isfinite(root), root, 0.0).amax(1)
-    s = torch.where(top >= 2.0 ** -100, top / 64516.0, 0.0)
+    s = torch.where(top >= 2.0 ** -100, top * (1.0 / 64516.0), 0.0)
     r = torch.where(s > 0, 1.0 / s, 0.0)
     q = torch.round(torch.sqrt(root * r[:, None]))
     q = torch.where(root > 0, q.clamp(min=1.0), q)
