@@ -307,6 +307,70 @@ int strads_release_cached(void);
 int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint64_t seed, uint64_t t,
                          int32_t n_candidates, uint32_t flags, int32_t* cand_dev, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * First-order steps.  (No counterpart in the paper: what its coordinate schedules are compared with, and how the layers
+ * around a sparse model are trained.)
+ *
+ * strads_adamw_step: one step of AdamW over `count` tensors at once, element by element
+ *     g <- grad_scale grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *     d = sqrt(v) / sqrt(1 - beta2^t) + eps;
+ *     p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / d;   p <- S(p, lr l1 / d)   (S as in Eq. 2; l1 = 0: not)
+ * The threshold is taken in the step's own metric d, so that a point where the step comes to rest satisfies the optimality
+ * conditions of Eq. 1 with lambda = l1.  Every element is a fixed sequence of correctly rounded binary32 operations; the
+ * scalars are formed in binary64 and rounded once.  Same inputs, same bits, however the tensors are aligned or listed.
+ *
+ * Types: parameters binary32, bfloat16 or binary16; gradients binary32 or the parameters' type; 16-bit parameters with or
+ * without a binary32 master copy (all tensors of a call or none), which then takes the step and is rounded to the parameter.
+ * Moments in 32 bits: m, v binary32 [n].  In 8 bits: a tensor is cut into blocks of STRADS_ADAMW_BLOCK elements (the last one
+ * may be shorter), m int8 [n] and v uint8 [n] with a binary32 scale each per block: m = s q |q| (q = -128: NaN),
+ * v = (s q^2)^2 (q = 255: NaN; a v that is not 0 is never stored as 0).  A block's scales are its largest finite |m| / 127^2
+ * and sqrt(v) / 254^2, or 0 where that magnitude is below 2^-100, which stores the block as noughts.  Codes go to the nearest,
+ * so a moment changes only when it moves by half a step of its code or its block's largest does.  All zeros (codes and
+ * scales) is the state before the first step.
+ * A gradient that is not finite makes its own element NaN and no other; skip_dev is how a program leaves such a step out.
+ *
+ * lr_dev, grad_scale_dev, step_dev, skip_dev: device addresses or NULL.  Where given, the value is read from there when
+ * the step runs, in place of the field of that name: a captured step follows its schedule.  *skip_dev != 0: the step changes
+ * nothing.  t = step or *step_dev counts from 1.
+ *
+ * Arrays are contiguous, aligned to their element; parameters, masters, moments and scales of all tensors are disjoint
+ * (shared parameters are refused; the rest is the caller's to keep).  n = 0 is allowed.  No workspace: the list travels with the
+ * launch, so it may be freed when the call returns, and a captured step keeps its own.  Asynchronous on `stream`, on the
+ * current device.
+ *
+ * strads_adamw_unpack: moments held in 8 bits as the binary32 values they stand for, m_out[i] and v_out[i] device [n_i]
+ * (params, masters and gradients of the list are not read). */
+#define STRADS_ADAMW_BLOCK 256
+typedef enum { STRADS_F32 = 0, STRADS_BF16 = 1, STRADS_F16 = 2 } strads_type_t;
+
+typedef struct {
+  void* param;
+  float* master;                        /* or NULL                                                */
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;                       /* 8 bits: [ceil(n / STRADS_ADAMW_BLOCK)]; 32 bits: ignored */
+  float* v_scale;
+  int64_t n;                            /* 0 <= n <= 2^40                                         */
+} strads_adamw_tensor_t;
+
+typedef struct {
+  int32_t param_type, grad_type;        /* strads_type_t                                          */
+  int32_t state_bits;                   /* 32 or 8                                                */
+  double  lr, beta1, beta2, eps;        /* lr >= 0, 0 <= beta < 1, eps > 0                        */
+  double  weight_decay, l1;             /* >= 0                                                   */
+  double  grad_scale;
+  int64_t step;                         /* t >= 1 (ignored with step_dev)                         */
+  const float*   lr_dev;
+  const float*   grad_scale_dev;
+  const int64_t* step_dev;
+  const int32_t* skip_dev;
+  void* stream;
+} strads_adamw_config_t;
+
+int strads_adamw_step(const strads_adamw_config_t* cfg, const strads_adamw_tensor_t* tensors, int32_t count);
+int strads_adamw_unpack(const strads_adamw_tensor_t* tensors, float* const* m_out, float* const* v_out, int32_t count, void* stream);
+
 const char* strads_error_string(int code);
 /* Text of the last CUDA error seen by this library on the calling thread ("" if none). */
 const char* strads_last_cuda_error(void);

@@ -35,6 +35,7 @@ EXPORTS = [
     "strads_set_round", "strads_totals", "strads_status", "strads_colnorm2", "strads_destroy",
     "strads_error_string", "strads_last_cuda_error", "strads_profile_begin", "strads_profile_end",
     "strads_sample_static", "strads_set_wait_limit", "strads_inject_stall", "strads_recover", "strads_margin", "strads_release_cached",
+    "strads_adamw_step", "strads_adamw_unpack",
 ]
 
 
@@ -58,6 +59,22 @@ class RoundOut(C.Structure):
     _fields_ = [("cand", C.c_void_p), ("kept", C.c_void_p), ("dbeta", C.c_void_p), ("counts", C.c_void_p),
                 ("gram", C.c_void_p)]
 
+
+class AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64)]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32),
+                ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("l1", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64),
+                ("lr_dev", C.c_void_p), ("grad_scale_dev", C.c_void_p), ("step_dev", C.c_void_p), ("skip_dev", C.c_void_p),
+                ("stream", C.c_void_p)]
+
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ADAMW_BLOCK = 256
 
 _lib = None
 
@@ -95,6 +112,9 @@ def load() -> C.CDLL:
         lib.strads_margin.argtypes = [C.c_void_p, C.POINTER(C.c_void_p)]
         lib.strads_sample_static.argtypes = [C.c_void_p, C.c_int64, C.c_float, C.c_uint64, C.c_uint64, C.c_int32,
                                              C.c_uint32, C.c_void_p, C.c_void_p]
+        lib.strads_adamw_step.argtypes = [C.POINTER(AdamWConfig), C.POINTER(AdamWTensor), C.c_int32]
+        lib.strads_adamw_unpack.argtypes = [C.POINTER(AdamWTensor), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int32,
+                                            C.c_void_p]
         lib.strads_profile_end.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         _lib = lib
     return _lib
@@ -308,3 +328,125 @@ class StradsLasso:
             self.close()
         except Exception:
             pass
+
+
+class AdamW:
+    """AdamW over many tensors at once, moments in 32 or in 8 bits (strads_adamw_step).
+
+    params are contiguous tensors of one type (float32, bfloat16, float16) on one CUDA device, stepped in place; masters,
+    with 16-bit parameters, their float32 copies, which then take the step.  moments, where given, are used as they are and
+    kept up to date: (first, second), lists of float32 tensors, with bits=32; (codes, scales, codes, scales), lists of
+    int8, float32, uint8 and float32 tensors, with bits=8 (a scale per block of 256 elements).  Otherwise they are allocated
+    here, as noughts.
+    """
+
+    def __init__(self, params, bits=32, masters=None, moments=None, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, l1=0.0):
+        params = list(params)
+        if bits not in (32, 8):
+            raise ValueError("bits must be 32 or 8")
+        if not params:
+            raise ValueError("no parameters")
+        dtype, dev = params[0].dtype, params[0].device
+        if dtype not in TYPES:
+            raise TypeError(f"parameters of type {dtype}")
+        if dev.type != "cuda":
+            raise ValueError("the parameters must live on a CUDA device")
+        if masters is not None and dtype == torch.float32:
+            raise ValueError("masters go with 16-bit parameters")
+        self.params, self.bits, self.device, self.dtype = params, bits, dev, dtype
+        self.masters = None if masters is None else list(masters)
+        sizes = [p.numel() for p in params]
+        blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+        if bits == 32:
+            kinds = [(torch.float32, sizes)] * 2
+        else:
+            kinds = [(torch.int8, sizes), (torch.float32, blocks), (torch.uint8, sizes), (torch.float32, blocks)]
+        if moments is None:
+            moments = [self._noughts(t, n, dev) for t, n in kinds]
+        self.state = [list(m) for m in moments]
+        if len(self.state) != len(kinds):
+            raise ValueError(f"{len(kinds)} lists of moments expected with {bits} bits")
+        self._check("parameters", params, dtype, sizes)
+        if self.masters is not None:
+            self._check("masters", self.masters, torch.float32, sizes)
+        for m, (t, n) in zip(self.state, kinds):
+            self._check("moments", m, t, n)
+        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                         for group in (params, self.masters or [], *self.state) for t in group if t.numel())
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise ValueError("parameters, masters and moments must not share memory")
+        self._cfg = AdamWConfig(param_type=TYPES[dtype], state_bits=bits, beta1=betas[0], beta2=betas[1], eps=eps,
+                                weight_decay=weight_decay, l1=l1)
+        self._list = (AdamWTensor * len(params))()
+        for i, p in enumerate(params):
+            e = self._list[i]
+            e.param, e.n = p.data_ptr(), p.numel()
+            e.master = self.masters[i].data_ptr() if self.masters is not None else None
+            e.m, e.v = self.state[0][i].data_ptr(), self.state[1 if bits == 32 else 2][i].data_ptr()
+            if bits == 8:
+                e.m_scale, e.v_scale = self.state[1][i].data_ptr(), self.state[3][i].data_ptr()
+
+    @staticmethod
+    def _noughts(dtype, sizes, dev):
+        starts, total = [], 0
+        for n in sizes:                                  # every tensor's part starts on 16 bytes
+            starts.append(total)
+            total += -(-n // 16) * 16
+        flat = torch.zeros(total, dtype=dtype, device=dev)
+        return [flat[a:a + n] for a, n in zip(starts, sizes)]
+
+    def _check(self, what, tensors, dtype, sizes):
+        if len(tensors) != len(sizes):
+            raise ValueError(f"{len(tensors)} {what} for {len(sizes)} parameters")
+        for t, n in zip(tensors, sizes):
+            if t.device != self.device or not t.is_contiguous() or t.numel() != n:
+                raise ValueError(f"{what} must be contiguous, of the parameters' sizes and on their device")
+            if t.dtype != dtype:
+                raise TypeError(f"{what} of type {t.dtype}, {dtype} expected")
+
+    def _scalar(self, t, dtype):
+        if t is None:
+            return None
+        if t.device != self.device or t.dtype != dtype or t.numel() != 1:
+            raise ValueError(f"a scalar on the device must be one {dtype} on {self.device}")
+        return t.data_ptr()
+
+    def step(self, grads, lr=1e-3, step=1, grad_scale=1.0, skip=None):
+        """One step with the given gradients (float32 or the parameters' type, contiguous).  `step` counts from 1.  lr (float32),
+        step (int64), grad_scale (float32) and skip (int32) may be one-element tensors on the device, read when the
+        step runs: a captured step then follows them; skip other than 0 leaves everything as it is."""
+        grads = list(grads)
+        gtype = grads[0].dtype if grads else None
+        if gtype not in (torch.float32, self.dtype):
+            raise TypeError(f"gradients of type {gtype}")
+        self._check("gradients", grads, gtype, [p.numel() for p in self.params])
+        c, on_device = self._cfg, lambda t: isinstance(t, torch.Tensor)
+        c.grad_type = TYPES[gtype]
+        c.lr_dev = self._scalar(lr, torch.float32) if on_device(lr) else None
+        c.step_dev = self._scalar(step, torch.int64) if on_device(step) else None
+        c.grad_scale_dev = self._scalar(grad_scale, torch.float32) if on_device(grad_scale) else None
+        c.skip_dev = self._scalar(skip, torch.int32)
+        c.lr, c.grad_scale, c.step = 0.0 if on_device(lr) else lr, 1.0 if on_device(grad_scale) else grad_scale, 1 if on_device(step) else step
+        for e, g in zip(self._list, grads):
+            e.grad = g.data_ptr()
+        with torch.cuda.device(self.device):
+            c.stream = torch.cuda.current_stream().cuda_stream
+            _check(load().strads_adamw_step(C.byref(c), self._list, len(grads)), "strads_adamw_step")
+
+    def moments(self, out=None):
+        """(first, second): the moments as lists of float32 tensors.  32 bits: the state itself.  8 bits: the values that the
+        codes stand for, in new tensors or in `out`, a pair of lists of contiguous float32 tensors."""
+        if self.bits == 32:
+            return self.state[0], self.state[1]
+        sizes = [p.numel() for p in self.params]
+        if out is None:
+            out = [self._noughts(torch.float32, sizes, self.device) for _ in range(2)]
+        first, second = (list(t) for t in out)
+        self._check("values", first, torch.float32, sizes)
+        self._check("values", second, torch.float32, sizes)
+        n = len(sizes)
+        ptrs = [(C.c_void_p * n)(*[t.data_ptr() or None for t in group]) for group in (first, second)]
+        with torch.cuda.device(self.device):
+            _check(load().strads_adamw_unpack(self._list, *ptrs, n, C.c_void_p(torch.cuda.current_stream().cuda_stream)),
+                   "strads_adamw_unpack")
+        return first, second

@@ -1379,3 +1379,7 @@ const char* strads_error_string(int code) {
 const char* strads_last_cuda_error(void) { return g_cuda_err; }
 
 }  // extern "C"
+
+namespace strads {
+int cuda_failed(cudaError_t e, const char* where) { return cuda_fail(e, where); }
+}  // namespace strads

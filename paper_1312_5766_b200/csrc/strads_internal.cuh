@@ -508,4 +508,8 @@ cudaError_t launch_set_counts(const Problem& p, int n_cand, int n_examined, int 
 struct Export { int* cand; int* kept; float* dbeta; int* counts; float* beta; float* delta; };
 cudaError_t launch_export(const Problem& p, const int* kept, const Export& to, cudaStream_t s);
 
+
+// Keeps the error's text for strads_last_cuda_error and returns STRADS_ERR_CUDA (entry points outside api.cu).
+int cuda_failed(cudaError_t e, const char* where);
+
 }  // namespace strads
