@@ -308,6 +308,63 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
                          int32_t n_candidates, uint32_t flags, int32_t* cand_dev, void* stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
+ * Linear layers: what one fitted model, or many at once, answer on given rows, the residuals that go with it, and the gradient.
+ *
+ * strads_linear_forward:   z = x w^T + bias,   out = residual + scale act(z)
+ *   x [n_rows][n_in], w [n_out][n_in], bias [n_out] or NULL, residual [n_rows][n_out] or NULL, out [n_rows][n_out]; preact
+ *   (or NULL) receives z.  With x a design matrix, the rows of w coefficient vectors (a path over lambda, several responses),
+ *   residual = y and scale = -1 it is the paper's residual y - X beta for each of them (Section 2.1), and with the sigmoid
+ *   y - sigma(X beta), the logistic loss's.
+ * strads_linear_backward:  from gout = dF/dout and the z kept by the forward pass (not read with the identity)
+ *   gz = scale gout act'(z),   gx = gz w,   gw = gz^T x,   gbias = column sums of gz     (each only where asked for)
+ *   dF/dresidual is gout itself.  act'(0) of the ReLU is 0.  n_rows = 0: gw and gbias are noughts.
+ *
+ * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more.  binary32 products go through three
+ * bfloat16 parts of each operand (24 bits together) on the tensor cores, or are formed as they are where one side has few
+ * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: gz is rounded to the type where the products
+ * read it (as a framework that keeps it would); z is rounded once, behind act.
+ * GELU is z Phi(z), GELU_TANH its tanh form 1/2 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), SILU z sigma(z).
+ *
+ * Matrices may have any strides (elements; >= 0 for what is read, so rows and columns may be repeated with stride 0; what is
+ * written must not overlap itself or any input, but out may be the residual itself).  Best are operands with one stride of 1,
+ * the other a multiple of 16 bytes and 16-byte aligned data, either order: these are read in place.  Others are first copied
+ * into the workspace, as are binary32 operands.
+ *
+ * The workspace (device, 256-byte aligned) holds nothing between calls; two calls that may run at the same time need one each.
+ * No allocation, no host synchronisation; may be captured.  Asynchronous on `stream`, on the current device, which must hold
+ * all arrays.  Same inputs, same bits.
+ * Should a bounded wait run out (see strads_set_wait_limit), the outputs are undefined and strads_linear_status says so:
+ * it waits for the device, and returns STRADS_OK or STRADS_ERR_TIMEOUT and the bits raised on the current device since the last
+ * call of it.  STRADS_LINEAR_FLAG_STALL withholds a call's operand loads, so that its waits run out after milliseconds. */
+typedef enum { STRADS_F32 = 0, STRADS_BF16 = 1, STRADS_F16 = 2 } strads_type_t;
+typedef enum {
+  STRADS_ACT_IDENTITY = 0, STRADS_ACT_RELU = 1, STRADS_ACT_SIGMOID = 2, STRADS_ACT_GELU = 3, STRADS_ACT_GELU_TANH = 4, STRADS_ACT_SILU = 5
+} strads_activation_t;
+#define STRADS_LINEAR_FLAG_STALL 1u
+
+typedef struct { const void* data; int64_t row_stride, col_stride; } strads_const_matrix_t;
+typedef struct { void* data; int64_t row_stride, col_stride; } strads_matrix_t;
+
+typedef struct {
+  int32_t type, activation;             /* strads_type_t, strads_activation_t                     */
+  int64_t n_rows, n_in, n_out;          /* 0 <= n_rows < 2^31, 1 <= n_in, n_out < 2^31             */
+  strads_const_matrix_t x, w;
+  float scale;
+  uint32_t flags;
+  void* workspace;                      /* 256-byte aligned, as long as the call's query says (NULL if that is 0) */
+  size_t workspace_bytes;
+  void* stream;
+} strads_linear_config_t;
+
+/* Workspace of a forward pass, and of a backward pass whatever it is asked for (workspace fields of cfg are not read). */
+int strads_linear_workspace_bytes(const strads_linear_config_t* cfg, size_t* forward_out, size_t* backward_out);
+int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, const strads_const_matrix_t* residual,
+                          const strads_matrix_t* out, const strads_matrix_t* preact);
+int strads_linear_backward(const strads_linear_config_t* cfg, const strads_const_matrix_t* gout, const strads_const_matrix_t* preact,
+                           const strads_matrix_t* gx, const strads_matrix_t* gw, void* gbias);
+int strads_linear_status(uint32_t* bits_host_out);
+
+/* ------------------------------------------------------------------------------------------------------------------
  * First-order steps.  (No counterpart in the paper: what its coordinate schedules are compared with, and how the layers
  * around a sparse model are trained.)
  *
@@ -341,8 +398,6 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  * strads_adamw_unpack: moments held in 8 bits as the binary32 values they stand for, m_out[i] and v_out[i] device [n_i]
  * (params, masters and gradients of the list are not read). */
 #define STRADS_ADAMW_BLOCK 256
-typedef enum { STRADS_F32 = 0, STRADS_BF16 = 1, STRADS_F16 = 2 } strads_type_t;
-
 typedef struct {
   void* param;
   float* master;                        /* or NULL                                                */

@@ -35,7 +35,8 @@ EXPORTS = [
     "strads_set_round", "strads_totals", "strads_status", "strads_colnorm2", "strads_destroy",
     "strads_error_string", "strads_last_cuda_error", "strads_profile_begin", "strads_profile_end",
     "strads_sample_static", "strads_set_wait_limit", "strads_inject_stall", "strads_recover", "strads_margin", "strads_release_cached",
-    "strads_adamw_step", "strads_adamw_unpack",
+    "strads_adamw_step", "strads_adamw_unpack", "strads_linear_workspace_bytes", "strads_linear_forward", "strads_linear_backward",
+    "strads_linear_status",
 ]
 
 
@@ -73,6 +74,18 @@ class AdamWConfig(C.Structure):
                 ("stream", C.c_void_p)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("col_stride", C.c_int64)]
+
+
+class LinearConfig(C.Structure):
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("n_rows", C.c_int64), ("n_in", C.c_int64), ("n_out", C.c_int64),
+                ("x", Matrix), ("w", Matrix), ("scale", C.c_float), ("flags", C.c_uint32), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+ACTIVATIONS = {"identity": 0, "relu": 1, "sigmoid": 2, "gelu": 3, "gelu_tanh": 4, "silu": 5}
+LINEAR_FLAG_STALL = 1
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ADAMW_BLOCK = 256
 
@@ -112,6 +125,10 @@ def load() -> C.CDLL:
         lib.strads_margin.argtypes = [C.c_void_p, C.POINTER(C.c_void_p)]
         lib.strads_sample_static.argtypes = [C.c_void_p, C.c_int64, C.c_float, C.c_uint64, C.c_uint64, C.c_int32,
                                              C.c_uint32, C.c_void_p, C.c_void_p]
+        lib.strads_linear_workspace_bytes.argtypes = [C.POINTER(LinearConfig), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        lib.strads_linear_forward.argtypes = [C.POINTER(LinearConfig), C.c_void_p] + [C.POINTER(Matrix)] * 3
+        lib.strads_linear_backward.argtypes = [C.POINTER(LinearConfig)] + [C.POINTER(Matrix)] * 4 + [C.c_void_p]
+        lib.strads_linear_status.argtypes = [C.POINTER(C.c_uint32)]
         lib.strads_adamw_step.argtypes = [C.POINTER(AdamWConfig), C.POINTER(AdamWTensor), C.c_int32]
         lib.strads_adamw_unpack.argtypes = [C.POINTER(AdamWTensor), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int32,
                                             C.c_void_p]
@@ -328,6 +345,109 @@ class StradsLasso:
             self.close()
         except Exception:
             pass
+
+
+def _matrix(t, what, like, shape):
+    """A tensor as the library takes it; refuses other types, devices and shapes than those of the call."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{what} of type {t.dtype}, {like.dtype} expected")
+    if t.device != like.device:
+        raise ValueError(f"{what} on {t.device}, {like.device} expected")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} of shape {tuple(t.shape)}, {tuple(shape)} expected")
+    return Matrix(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _linear_config(x, w, activation, scale, flags):
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must have two dimensions")
+    if x.device.type != "cuda":
+        raise ValueError("x must live on a CUDA device")
+    if x.dtype not in TYPES:
+        raise TypeError(f"x of type {x.dtype}")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
+    (n, k), m = x.shape, w.shape[0]
+    cfg = LinearConfig(type=TYPES[x.dtype], activation=ACTIVATIONS[activation], n_rows=n, n_in=k, n_out=m, scale=scale, flags=flags)
+    cfg.x, cfg.w = _matrix(x, "x", x, (n, k)), _matrix(w, "w", x, (m, k))
+    return cfg
+
+
+def _linear_workspace(cfg, which, device):
+    """The call's workspace: from the caching allocator, on the current stream, so that no two calls share one unless they follow each other."""
+    need = (C.c_size_t * 2)()
+    _check(load().strads_linear_workspace_bytes(C.byref(cfg), C.cast(C.byref(need, 0), C.POINTER(C.c_size_t)),
+                                                C.cast(C.byref(need, C.sizeof(C.c_size_t)), C.POINTER(C.c_size_t))), "strads_linear_workspace_bytes")
+    ws = torch.empty(need[which], dtype=torch.uint8, device=device) if need[which] else None
+    cfg.workspace, cfg.workspace_bytes = (ws.data_ptr() if ws is not None else None), need[which]
+    cfg.stream = torch.cuda.current_stream().cuda_stream
+    return ws
+
+
+def _vector(t, what, like, n):
+    if t.dtype != like.dtype:
+        raise TypeError(f"{what} of type {t.dtype}, {like.dtype} expected")
+    if t.device != like.device or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous, of shape ({n},) and on {like.device}")
+    return C.c_void_p(t.data_ptr())
+
+
+def linear_forward(x, w, bias=None, residual=None, activation="identity", scale=1.0, want_preact=False, out=None, preact=None, flags=0):
+    """out = residual + scale * activation(x w^T + bias) (strads_linear_forward).  x [n_rows, n_in] and w [n_out, n_in] in either
+    order, float32, bfloat16 or float16; residual [n_rows, n_out] may be an expanded tensor, and out may be the residual itself.
+    Returns out, and with want_preact (or preact, a tensor for it) the pair (out, x w^T + bias)."""
+    cfg = _linear_config(x, w, activation, scale, flags)
+    shape = (cfg.n_rows, cfg.n_out)
+    b = None if bias is None else _vector(bias, "bias", x, cfg.n_out)
+    r = None if residual is None else C.byref(_matrix(residual, "residual", x, shape))
+    with torch.cuda.device(x.device):
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        if preact is None and want_preact:
+            preact = torch.empty(shape, dtype=x.dtype, device=x.device)
+        o = _matrix(out, "out", x, shape)
+        z = None if preact is None else C.byref(_matrix(preact, "preact", x, shape))
+        ws = _linear_workspace(cfg, 0, x.device)
+        _check(load().strads_linear_forward(C.byref(cfg), b, r, C.byref(o), z), "strads_linear_forward")
+    del ws
+    return out if preact is None else (out, preact)
+
+
+def linear_backward(grad_out, x, w, preact=None, activation="identity", scale=1.0, want_x=True, want_w=True, want_bias=True,
+                    grad_x=None, grad_w=None, grad_bias=None, flags=0):
+    """Gradients of linear_forward (strads_linear_backward) from grad_out [n_rows, n_out] and the preact that the forward pass gave
+    (not with the identity): (grad_x, grad_w, grad_bias), None where not wanted.  New gradients have the order of x and w.  The residual's
+    gradient is grad_out itself."""
+    cfg = _linear_config(x, w, activation, scale, flags)
+    shape = (cfg.n_rows, cfg.n_out)
+    g = _matrix(grad_out, "grad_out", x, shape)
+    if activation != "identity" and preact is None:
+        raise ValueError("the gradient needs preact")
+    z = None if preact is None else C.byref(_matrix(preact, "preact", x, shape))
+    like = lambda t: torch.empty(t.shape[::-1], dtype=t.dtype, device=t.device).t() if t.stride(0) < t.stride(1) else \
+        torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    with torch.cuda.device(x.device):
+        if want_x and grad_x is None:
+            grad_x = like(x)
+        if want_w and grad_w is None:
+            grad_w = like(w)
+        if want_bias and grad_bias is None:
+            grad_bias = torch.empty(cfg.n_out, dtype=x.dtype, device=x.device)
+        gx = None if grad_x is None else C.byref(_matrix(grad_x, "grad_x", x, x.shape))
+        gw = None if grad_w is None else C.byref(_matrix(grad_w, "grad_w", x, w.shape))
+        gb = None if grad_bias is None else _vector(grad_bias, "grad_bias", x, cfg.n_out)
+        ws = _linear_workspace(cfg, 1, x.device)
+        _check(load().strads_linear_backward(C.byref(cfg), C.byref(g), z, gx, gw, gb), "strads_linear_backward")
+    del ws
+    return grad_x, grad_w, grad_bias
+
+
+def linear_status(device=None) -> tuple[int, int]:
+    """(code, bits) of the linear layers' bounded waits on a device since the last call of this (waits for the device)."""
+    bits = C.c_uint32(0)
+    with torch.cuda.device(device):
+        rc = load().strads_linear_status(C.byref(bits))
+    return rc, int(bits.value)
 
 
 class AdamW:
