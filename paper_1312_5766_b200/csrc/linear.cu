@@ -1,69 +1,311 @@
-// Linear layers: out = residual + scale act(x w^T + bias) and its gradient.  Argument checks, workspace, and which kernel
-// forms which product.
+// Linear layers: out = residual + scale act(x w^T + bias) and its gradient.  Argument checks, workspace, the passes that bring
+// operands into the form that the products read, and which kernel forms which product.
 #include <cmath>
 
-#include "linear.cuh"
+#include "linear_tc.cuh"
 
 namespace strads {
 namespace {
 
 __device__ unsigned int g_linear_status;       // STRADS_STATUS_* bits of the layers' bounded waits
 
-// ---- products, one 64 x 64 tile of D per CTA, any strides ----
-constexpr int kTile = 64, kDepth = 16;
-template <typename TA, typename TB, typename T>
-__global__ void __launch_bounds__(256) k_linear_simple(Operand A, Operand B, long long na, long long nb, long long nk, Finish f) {
-  __shared__ float sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
-  const int t = threadIdx.x, ta = t % 16, tb = t / 16;
-  const long long a0 = (long long)blockIdx.x * kTile, b0 = (long long)blockIdx.y * kTile;
-  float acc[4][4] = {};
-  for (long long k0 = 0; k0 < nk; k0 += kDepth) {
-    for (int i = t; i < kTile * kDepth; i += 256) {
-      const int ra = A.ks == 1 ? i / kDepth : i % kTile, ka = A.ks == 1 ? i % kDepth : i / kTile;
-      const int rb = B.ks == 1 ? i / kDepth : i % kTile, kb = B.ks == 1 ? i % kDepth : i / kTile;
-      sa[ka][ra] = a0 + ra < na && k0 + ka < nk ? load_f32(static_cast<const TA*>(A.p) + (a0 + ra) * A.rs + (k0 + ka) * A.ks) : 0.f;
-      sb[kb][rb] = b0 + rb < nb && k0 + kb < nk ? load_f32(static_cast<const TB*>(B.p) + (b0 + rb) * B.rs + (k0 + kb) * B.ks) : 0.f;
+constexpr int kThreads = 256;
+
+// ---- operands of the tensor-core products that cannot be read in place ----
+// dst[plane][outer][ld] from src, eight neighbours per thread.  binary32: x = p0 + p1 + p2, each the nearest bfloat16 to what is left
+// (24 bits together; where the nearest would be infinite, the next towards 0); what is not finite stays in p0 alone.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long long outer_stride, long long inner_stride, long long outer, long long inner,
+                                                          unsigned short* dst, long long ld, long long plane, int vec) {
+  chain_begin();
+  const long long per = ld / 8, total = outer * per;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < total; i += (long long)gridDim.x * kThreads) {
+    const long long o = i / per, k = i % per * 8;
+    const T* at = src + o * outer_stride + k * inner_stride;
+    __align__(16) T x[8];
+    if (vec && k + 8 <= inner) {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(x)[j] = __ldg(reinterpret_cast<const uint4*>(at) + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) if (k + j < inner) x[j] = at[j * inner_stride];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) if (k + j >= inner) store_f32(&x[j], 0.f);
     }
-    __syncthreads();
+    unsigned short* to = dst + o * ld + k;
+    if (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
+    } else {
+      __align__(16) __nv_bfloat16 p[3][8];
 #pragma unroll
-    for (int k = 0; k < kDepth; ++k)
+      for (int j = 0; j < 8; ++j) {
+        const float v = load_f32(&x[j]);
+        const bool finite = fabsf(v) <= 3.402823466e38f;
+        float h = __bfloat162float(__float2bfloat16_rn(v));
+        if (finite && fabsf(h) > 3.402823466e38f) h = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+        const float r1 = finite ? v - h : 0.f, m = __bfloat162float(__float2bfloat16_rn(r1));
+        p[0][j] = __float2bfloat16_rn(h);
+        p[1][j] = __float2bfloat16_rn(r1);
+        p[2][j] = __float2bfloat16_rn(r1 - m);
+      }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ta + 16 * i], sb[k][tb + 16 * j], acc[i][j]);
-    __syncthreads();
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + q * plane) = *reinterpret_cast<const uint4*>(p[q]);
+    }
   }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const long long a = a0 + ta + 16 * i, b = b0 + tb + 16 * j;
-      if (a < na && b < nb) finish<T>(f, acc[i][j], a, b);
-    }
 }
 
-// gz[n][m] = scale gout act'(preact), binary32.
+// ---- gz = scale gout act'(preact), and its column sums ----
+// A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row.  gz (may be null) [n][ld], rounded to T;
+// partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
 template <typename T>
-__global__ void k_linear_slope(Operand gout, Operand preact, long long n, long long m, int act, float scale, float* gz) {
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n * m; i += (long long)gridDim.x * blockDim.x) {
-    const long long r = i / m, c = i % m;
-    float g = scale * load_f32(static_cast<const T*>(gout.p) + r * gout.rs + c * gout.ks);
-    if (act != STRADS_ACT_IDENTITY) g *= slope(load_f32(static_cast<const T*>(preact.p) + r * preact.rs + c * preact.ks), act);
-    gz[i] = g;
+__global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand preact, long long n, long long m, int act, float scale, T* gz, long long ld,
+                                                        float* partial, long long rows, int vec) {
+  __shared__ float sum[8][256 + 8];
+  chain_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
+  float total[8] = {};
+  for (long long r = r0 + warp; r < r1; r += 8) {
+    __align__(16) T g[8], z[8];
+    const T *gp = static_cast<const T*>(gout.p) + r * gout.rs + c * gout.ks, *zp = static_cast<const T*>(preact.p) + r * preact.rs + c * preact.ks;
+    if (vec && c + 8 <= m) {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(g)[j] = __ldg(reinterpret_cast<const uint4*>(gp) + j);
+      if (act != STRADS_ACT_IDENTITY)
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(z)[j] = __ldg(reinterpret_cast<const uint4*>(zp) + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        store_f32(&g[j], 0.f);
+        store_f32(&z[j], 0.f);
+        if (c + j < m) {
+          g[j] = gp[j * gout.ks];
+          if (act != STRADS_ACT_IDENTITY) z[j] = zp[j * preact.ks];
+        }
+      }
+    }
+    __align__(16) T out[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float v = scale * load_f32(&g[j]);
+      if (act != STRADS_ACT_IDENTITY) v *= slope(load_f32(&z[j]), act);
+      total[j] += v;
+      store_f32(&out[j], v);
+    }
+    if (gz != nullptr && c < m) {                        // (ld is a multiple of 8: the last group has its place)
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(gz + r * ld + c)[j] = reinterpret_cast<const uint4*>(out)[j];
+    }
+  }
+  if (partial == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[warp][j * 33 + lane] = total[j];
+  __syncthreads();
+  const long long col = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (col < m) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += sum[w][(threadIdx.x & 7) * 33 + (threadIdx.x >> 3)];
+    partial[(long long)blockIdx.y * m + col] = v;
   }
 }
 template <typename T>
-__global__ void k_linear_bias_grad(const float* gz, long long n, long long m, T* gbias) {
-  const long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+__global__ void __launch_bounds__(kThreads) k_linear_bias_grad(const float* partial, int blocks, long long m, T* gbias) {
+  chain_begin();
+  const long long c = (long long)blockIdx.x * kThreads + threadIdx.x;
   if (c >= m) return;
   float s = 0.f;
-  for (long long r = 0; r < n; ++r) s += gz[r * m + c];
+#pragma unroll 8
+  for (int r = 0; r < blocks; ++r) s += partial[r * m + c];
   store_f32(gbias + c, s);
 }
 
-template <typename TA, typename TB, typename T>
-cudaError_t product(const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s) {
-  const dim3 grid((unsigned)((na + kTile - 1) / kTile), (unsigned)((nb + kTile - 1) / kTile));
-  k_linear_simple<TA, TB, T><<<grid, 256, 0, s>>>(A, B, na, nb, nk, f);
-  return cudaGetLastError();
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_linear_zero(T* p, long long rows, long long cols, long long rs, long long cs) {
+  chain_begin();
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < rows * cols; i += (long long)gridDim.x * kThreads)
+    store_f32(p + i / cols * rs + i % cols * cs, 0.f);
+}
+
+// ---- the order of kernels ----
+// A call is gone through twice by the same code: with s.run false to add up the workspace, then to launch.
+struct Call {
+  int type;
+  size_t size;                           // of an element
+  char* ws;
+  size_t used;
+  bool run, stall;
+  cudaStream_t stream;
+  cudaError_t err;
+  unsigned int* status;
+  void* take(size_t bytes) {
+    void* p = ws + used;
+    used += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+constexpr int kGrid = 148 * 8;           // CTAs of the passes over an operand: enough to keep the memory busy
+
+unsigned ctas_for(long long groups) {
+  const long long n = (groups + kThreads - 1) / kThreads;
+  return (unsigned)(n < 1 ? 1 : n > kGrid ? kGrid : n);
+}
+bool vec_rows(const void* p, long long pitch, long long rows, size_t size) {
+  return ((uintptr_t)p & 15) == 0 && (rows == 1 || (pitch * (long long)size) % 16 == 0);
+}
+
+// `unknown`: where the matrix lies is not known yet (a workspace query), so that it has to be taken for one that is copied.
+Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unknown = false) {
+  const bool rows_inner = m.ks != 1 && (m.rs == 1 || rows == 1) && nk > 1;
+  Planes p = {};
+  p.rows_inner = rows_inner;
+  p.inner = rows_inner ? rows : nk;
+  p.outer = rows_inner ? nk : rows;
+  const long long outer_stride = rows_inner ? m.ks : m.rs, inner_stride = rows_inner ? m.rs : m.ks;
+  p.planes = c.size == 4 ? 3 : 1;
+  if (!unknown && c.size == 2 && (inner_stride == 1 || p.inner == 1) && ((uintptr_t)m.p & 15) == 0 && (p.outer == 1 || (outer_stride % 8 == 0 && outer_stride >= p.inner))) {
+    p.p = m.p;
+    p.ld = p.outer == 1 ? (p.inner + 7) / 8 * 8 : outer_stride;
+    return p;
+  }
+  p.ld = (p.inner + 7) / 8 * 8;
+  p.plane = p.outer * p.ld;
+  void* dst = c.take((size_t)p.plane * p.planes * 2);
+  p.p = dst;
+  if (!c.run || c.err != cudaSuccess) return p;
+  const int vec = (inner_stride == 1) && vec_rows(m.p, outer_stride, p.outer, c.size);
+  const unsigned grid = ctas_for(p.plane / 8);
+  unsigned short* to = static_cast<unsigned short*>(dst);
+  c.err = c.size == 4 ? launch_chained(k_linear_pack<float>, grid, kThreads, 0, c.stream, static_cast<const float*>(m.p), outer_stride, inner_stride, p.outer, p.inner, to, p.ld, p.plane, vec)
+                      : launch_chained(k_linear_pack<__half>, grid, kThreads, 0, c.stream, static_cast<const __half*>(m.p), outer_stride, inner_stride, p.outer, p.inner, to, p.ld, p.plane, vec);
+  return p;
+}
+
+// A matrix as one side of products, brought into the workspace at most once: the other side of its transpose is the same copy.
+struct Matrix {
+  Operand m;                             // element (row, column)
+  long long rows, cols;
+  bool unknown, brought;
+  Planes p;
+};
+Operand operand_of(const strads_const_matrix_t& m) { return Operand{m.data, (long long)m.row_stride, (long long)m.col_stride}; }
+Matrix matrix_of(const Operand& m, long long rows, long long cols) {
+  Matrix x = {};
+  x.m = m; x.rows = rows; x.cols = cols;
+  return x;
+}
+Planes side_of(Call& c, Matrix& x, bool columns_as_rows) {
+  if (!x.brought) { x.p = bring(c, x.m, x.rows, x.cols, x.unknown); x.brought = true; }
+  Planes p = x.p;
+  if (columns_as_rows) p.rows_inner = !p.rows_inner;
+  return p;
+}
+
+// D = A B^T, A and B matrices or (t) their transposes.
+void product(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
+  const Operand a = ta ? Operand{A.m.p, A.m.ks, A.m.rs} : A.m, b = tb ? Operand{B.m.p, B.m.ks, B.m.rs} : B.m;
+  const long long na = ta ? A.cols : A.rows, nb = tb ? B.cols : B.rows, nk = ta ? A.rows : A.cols;
+  if ((na < nb ? na : nb) <= kThinMost) {
+    if (c.run && c.err == cudaSuccess) c.err = launch_linear_thin(c.type, a, b, na, nb, nk, f, c.stream);
+    return;
+  }
+  const Planes pa = side_of(c, A, ta), pb = side_of(c, B, tb);
+  if (c.run && c.err == cudaSuccess) c.err = launch_linear_tc(c.type, pa, pb, na, nb, nk, f, c.status, c.stall, c.stream);
+}
+
+Side side(const void* p, long long rs, long long cs, bool a_is_rows) { return a_is_rows ? Side{p, rs, cs} : Side{p, cs, rs}; }
+// Which of D's sides runs through memory (the rows only where the columns do not).
+bool rows_run(long long rs, long long cs) { return cs != 1 && rs == 1; }
+
+void forward(Call& c, const strads_linear_config_t& g, const void* bias, const strads_const_matrix_t* residual, const strads_matrix_t* out,
+             const strads_matrix_t* preact) {
+  Matrix x = matrix_of(operand_of(g.x), g.n_rows, g.n_in), w = matrix_of(operand_of(g.w), g.n_out, g.n_in);
+  Finish f = {};
+  f.act = g.activation; f.scale = g.scale; f.bias = bias;
+  bool ar = false;
+  if (out != nullptr) {
+    ar = rows_run(out->row_stride, out->col_stride);
+    f.out = side(out->data, out->row_stride, out->col_stride, ar);
+  }
+  if (residual) f.residual = side(residual->data, residual->row_stride, residual->col_stride, ar);
+  if (preact) f.preact = side(preact->data, preact->row_stride, preact->col_stride, ar);
+  f.bias_a = ar ? 0 : 1; f.bias_b = ar ? 1 : 0;
+  f.plain = g.activation == STRADS_ACT_IDENTITY && bias == nullptr && residual == nullptr && preact == nullptr;
+  if (ar) product(c, x, false, w, false, f); else product(c, w, false, x, false, f);
+}
+
+template <typename T>
+void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, T* gz, long long ld, T* gbias) {
+  long long rows = (g.n_rows + 127) / 128;                              // at most 128 blocks of rows, of at least 64 and a multiple of 8
+  rows = rows < 64 ? 64 : (rows + 7) / 8 * 8;
+  const int blocks = (int)((g.n_rows + rows - 1) / rows);
+  float* partial = gbias != nullptr || !c.run ? static_cast<float*>(c.take((size_t)blocks * (size_t)g.n_out * sizeof(float))) : nullptr;
+  if (!c.run || c.err != cudaSuccess) return;
+  const Operand o = operand_of(gout);
+  Operand z = {};
+  if (preact) z = operand_of(*preact);
+  const int vec = gout.col_stride == 1 && vec_rows(gout.data, gout.row_stride, g.n_rows, sizeof(T)) &&
+                  (g.activation == STRADS_ACT_IDENTITY || (z.ks == 1 && vec_rows(z.p, z.rs, g.n_rows, sizeof(T))));
+  c.err = launch_chained(k_linear_gz<T>, dim3((unsigned)((g.n_out + 255) / 256), (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
+                         (int)g.activation, g.scale, gz, ld, partial, rows, vec);
+  if (gbias != nullptr && c.err == cudaSuccess)
+    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + kThreads - 1) / kThreads)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, gbias);
+}
+
+template <typename T>
+void backward(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, const strads_matrix_t* gx,
+              const strads_matrix_t* gw, void* gbias) {
+  if (g.n_rows == 0) {
+    if (!c.run) return;
+    if (gw != nullptr)
+      c.err = launch_chained(k_linear_zero<T>, ctas_for(g.n_out * g.n_in), kThreads, 0, c.stream, static_cast<T*>(gw->data), (long long)g.n_out, (long long)g.n_in, (long long)gw->row_stride, (long long)gw->col_stride);
+    if (gbias != nullptr && c.err == cudaSuccess)
+      c.err = launch_chained(k_linear_zero<T>, ctas_for(g.n_out), kThreads, 0, c.stream, static_cast<T*>(gbias), 1ll, (long long)g.n_out, (long long)g.n_out, 1ll);
+    return;
+  }
+  // the identity's gz is gout itself, its scale a factor of the results; otherwise gz is formed, and its column sums on the way
+  const bool formed = g.activation != STRADS_ACT_IDENTITY;
+  const long long ld = (g.n_out + 7) / 8 * 8;
+  T* gz = formed ? static_cast<T*>(c.take((size_t)g.n_rows * (size_t)ld * sizeof(T))) : nullptr;
+  if (formed || gbias != nullptr || !c.run) gradient_of_z<T>(c, g, gout, preact, gz, ld, static_cast<T*>(gbias));
+  Operand kept = operand_of(gout);
+  if (formed) { kept.p = gz; kept.rs = ld; kept.ks = 1; }
+  Matrix z = matrix_of(kept, g.n_rows, g.n_out), x = matrix_of(operand_of(g.x), g.n_rows, g.n_in), w = matrix_of(operand_of(g.w), g.n_out, g.n_in);
+  z.unknown = !formed && !c.run;
+  Finish f = {};
+  f.plain = 1;
+  f.scale = formed ? 1.f : g.scale;
+  if (gx != nullptr || !c.run) {
+    const bool ar = gx != nullptr && rows_run(gx->row_stride, gx->col_stride);
+    if (gx != nullptr) f.out = side(gx->data, gx->row_stride, gx->col_stride, ar);
+    if (ar) product(c, z, false, w, true, f); else product(c, w, true, z, false, f);
+  }
+  if (gw != nullptr || !c.run) {
+    const bool ar = gw != nullptr && rows_run(gw->row_stride, gw->col_stride);
+    if (gw != nullptr) f.out = side(gw->data, gw->row_stride, gw->col_stride, ar);
+    if (ar) product(c, z, true, x, true, f); else product(c, x, true, z, true, f);
+  }
+}
+void backward_of(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, const strads_matrix_t* gx,
+                 const strads_matrix_t* gw, void* gbias) {
+  if (g.type == STRADS_F32) backward<float>(c, g, gout, preact, gx, gw, gbias);
+  else if (g.type == STRADS_BF16) backward<__nv_bfloat16>(c, g, gout, preact, gx, gw, gbias);
+  else backward<__half>(c, g, gout, preact, gx, gw, gbias);
+}
+Call call_of(const strads_linear_config_t& g, bool run) {
+  Call c = {};
+  c.type = g.type; c.size = g.type == STRADS_F32 ? 4 : 2;
+  c.run = run; c.stall = (g.flags & STRADS_LINEAR_FLAG_STALL) != 0;
+  c.ws = run ? static_cast<char*>(g.workspace) : nullptr;
+  c.stream = static_cast<cudaStream_t>(g.stream);
+  c.err = cudaSuccess;
+  if (run) {
+    void* p = nullptr;
+    c.err = cudaGetSymbolAddress(&p, g_linear_status);
+    c.status = static_cast<unsigned int*>(p);
+  }
+  return c;
 }
 
 bool valid_strides(long long rs, long long cs) { return rs >= 0 && cs >= 0; }
@@ -90,47 +332,6 @@ int check(const strads_linear_config_t& c) {
   return STRADS_OK;
 }
 
-template <typename T>
-cudaError_t forward(const strads_linear_config_t& c, const void* bias, const strads_const_matrix_t* residual, const strads_matrix_t& out,
-                    const strads_matrix_t* preact, cudaStream_t s) {
-  Finish f = {};
-  f.act = c.activation; f.scale = c.scale;
-  f.plain = 0;
-  f.bias = bias;
-  f.bias_a = 1;
-  f.out = {out.data, out.col_stride, out.row_stride};
-  if (residual) f.residual = {residual->data, residual->col_stride, residual->row_stride};
-  if (preact) f.preact = {preact->data, preact->col_stride, preact->row_stride};
-  return product<T, T, T>({c.w.data, c.w.row_stride, c.w.col_stride}, {c.x.data, c.x.row_stride, c.x.col_stride}, c.n_out, c.n_rows, c.n_in, f, s);
-}
-
-template <typename T>
-cudaError_t backward(const strads_linear_config_t& c, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, const strads_matrix_t* gx,
-                     const strads_matrix_t* gw, void* gbias, cudaStream_t s) {
-  float* gz = static_cast<float*>(c.workspace);
-  const Operand z = preact ? Operand{preact->data, preact->row_stride, preact->col_stride} : Operand{};
-  cudaError_t e = cudaSuccess;
-  if (c.n_rows > 0) {
-    k_linear_slope<T><<<1184, 256, 0, s>>>({gout.data, gout.row_stride, gout.col_stride}, z, c.n_rows, c.n_out, c.activation, c.scale, gz);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  }
-  Finish f = {};
-  f.plain = 1;
-  if (gx != nullptr && c.n_rows > 0) {
-    f.out = {gx->data, gx->col_stride, gx->row_stride};
-    if ((e = product<T, float, T>({c.w.data, c.w.col_stride, c.w.row_stride}, {gz, c.n_out, 1}, c.n_in, c.n_rows, c.n_out, f, s)) != cudaSuccess) return e;
-  }
-  if (gw != nullptr) {
-    f.out = {gw->data, gw->col_stride, gw->row_stride};
-    if ((e = product<T, float, T>({c.x.data, c.x.col_stride, c.x.row_stride}, {gz, 1, c.n_out}, c.n_in, c.n_out, c.n_rows, f, s)) != cudaSuccess) return e;
-  }
-  if (gbias != nullptr) {
-    k_linear_bias_grad<T><<<(unsigned)((c.n_out + 255) / 256), 256, 0, s>>>(gz, c.n_rows, c.n_out, static_cast<T*>(gbias));
-    e = cudaGetLastError();
-  }
-  return e;
-}
-
 }  // namespace
 }  // namespace strads
 
@@ -142,8 +343,13 @@ int strads_linear_workspace_bytes(const strads_linear_config_t* cfg, size_t* for
   if (cfg == nullptr || forward_out == nullptr || backward_out == nullptr) return STRADS_ERR_INVALID_ARG;
   const int rc = check(*cfg);
   if (rc != STRADS_OK) return rc;
-  *forward_out = 0;
-  *backward_out = (size_t)cfg->n_rows * (size_t)cfg->n_out * sizeof(float);
+  Call f = call_of(*cfg, false), b = call_of(*cfg, false);
+  if (cfg->n_rows > 0) {
+    forward(f, *cfg, nullptr, nullptr, nullptr, nullptr);
+    backward_of(b, *cfg, strads_const_matrix_t{nullptr, 0, 0}, nullptr, nullptr, nullptr, nullptr);
+  }
+  *forward_out = f.used;
+  *backward_out = b.used;
   return STRADS_OK;
 }
 
@@ -167,11 +373,9 @@ int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, c
   if (out == nullptr || !valid_out(*out, size, c.n_rows, c.n_out) || (preact != nullptr && !valid_out(*preact, size, c.n_rows, c.n_out)) ||
       (residual != nullptr && !valid_in(*residual, size)) || ((uintptr_t)bias % size) != 0)
     return STRADS_ERR_INVALID_ARG;
-  const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
-  const cudaError_t e = c.type == STRADS_F32 ? forward<float>(c, bias, residual, *out, preact, s)
-                      : c.type == STRADS_BF16 ? forward<__nv_bfloat16>(c, bias, residual, *out, preact, s)
-                                              : forward<__half>(c, bias, residual, *out, preact, s);
-  return e == cudaSuccess ? STRADS_OK : cuda_failed(e, "strads_linear_forward");
+  Call call = call_of(c, true);
+  forward(call, c, bias, residual, out, preact);
+  return call.err == cudaSuccess ? STRADS_OK : cuda_failed(call.err, "strads_linear_forward");
 }
 
 int strads_linear_backward(const strads_linear_config_t* cfg, const strads_const_matrix_t* gout, const strads_const_matrix_t* preact,
@@ -190,11 +394,9 @@ int strads_linear_backward(const strads_linear_config_t* cfg, const strads_const
   if (gx == nullptr && gw == nullptr && gbias == nullptr) return STRADS_OK;
   const strads_const_matrix_t none = {nullptr, 0, 0};
   const strads_const_matrix_t& g = gout ? *gout : none;
-  const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
-  const cudaError_t e = c.type == STRADS_F32 ? backward<float>(c, g, preact, gx, gw, gbias, s)
-                      : c.type == STRADS_BF16 ? backward<__nv_bfloat16>(c, g, preact, gx, gw, gbias, s)
-                                              : backward<__half>(c, g, preact, gx, gw, gbias, s);
-  return e == cudaSuccess ? STRADS_OK : cuda_failed(e, "strads_linear_backward");
+  Call call = call_of(c, true);
+  backward_of(call, c, g, preact, gx, gw, gbias);
+  return call.err == cudaSuccess ? STRADS_OK : cuda_failed(call.err, "strads_linear_backward");
 }
 
 int strads_linear_status(uint32_t* bits_host_out) {

@@ -18,7 +18,7 @@ struct Finish {
   long long bias_a, bias_b;
   int act;
   float scale;
-  int plain;                                                          // no bias, activation, residual, preact; scale 1
+  int plain;                                                          // no bias, activation, residual, preact
 };
 
 __device__ __forceinline__ float load_f32(const float* p) { return *p; }
@@ -55,10 +55,34 @@ __device__ __forceinline__ float slope(float z, int act) {
   }
 }
 
+// The same for several values: one branch for all of them.
+template <int kN>
+__device__ __forceinline__ void activate_all(float (&v)[kN], int act) {
+  if (act == STRADS_ACT_IDENTITY) return;
+  if (act == STRADS_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_RELU);
+  } else if (act == STRADS_ACT_SIGMOID) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_SIGMOID);
+  } else if (act == STRADS_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_GELU);
+  } else if (act == STRADS_ACT_GELU_TANH) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_GELU_TANH);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_SILU);
+  }
+}
+
 // One element of D.
 template <typename T>
 __device__ __forceinline__ void finish(const Finish& f, float z, long long a, long long b) {
-  if (!f.plain) {
+  if (f.plain) {
+    z *= f.scale;
+  } else {
     if (f.bias) z += load_f32(static_cast<const T*>(f.bias) + a * f.bias_a + b * f.bias_b);
     if (f.preact.p) store_f32(static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + b * f.preact.sb, z);
     z = f.scale * activate(z, f.act);
@@ -66,5 +90,10 @@ __device__ __forceinline__ void finish(const Finish& f, float z, long long a, lo
   }
   store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + b * f.out.sb, z);
 }
+
+// ---- products with few rows on one side (linear_thin.cu) ----
+// D = A B^T with nb <= kThinMost rows in B, or in A (then swapped): every element of the long side is read once, from where it is.
+constexpr int kThinMost = 8;
+cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s);
 
 }  // namespace strads

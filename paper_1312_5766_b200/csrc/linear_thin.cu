@@ -1,0 +1,255 @@
+// Products of linear layers with few rows on one side: the margins of one or a few fits, a gradient for one response, a layer
+// for single tokens.  Bound by reading the long operand once.  Plain FP32 multiply-adds, no copy of the operand, no tensor
+// cores: a tile of theirs would be nearly empty, and binary32 would have to be split first.
+//
+//   k along memory (k_thin_k): a warp takes rows, a lane every 32nd group of 16 bytes of them; lanes are added by shuffles.
+//   rows along memory (k_thin_rows): a lane takes the rows of 16 bytes, a warp every eighth k; warps are added through shared memory.
+//
+// The short side is staged in shared memory as binary32.  Where the rows alone do not fill the GPU, the CTAs of a cluster share k
+// and add through distributed shared memory, in the order of the CTAs.
+#include <mutex>
+
+#include "linear.cuh"
+
+namespace strads {
+namespace {
+
+constexpr int kThreads = 256, kWarps = 8;
+constexpr int kStageFloats = 8192;             // of the short side in shared memory at a time
+
+struct Thin {
+  Operand L, S;                                // the long and the short side
+  long long nl, nk;
+  int ns, splits, swapped, vec;                // swapped: the long side is D's b
+  int wk;                                      // k_thin_k: warps of a CTA that share a row's k (1 or 8)
+  Finish f;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float load_peer(const float* p, uint32_t rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+template <typename T>
+__device__ __forceinline__ void finish_thin(const Thin& t, float v, long long l, int s) {
+  if (t.swapped) finish<T>(t.f, v, s, l); else finish<T>(t.f, v, l, s);
+}
+
+// 16 bytes of T as floats.
+template <typename T> struct Vec { static constexpr int kN = 16 / sizeof(T); T x[kN]; };
+template <typename T>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[16 / sizeof(T)]) {
+  const uint4 raw = __ldg(reinterpret_cast<const uint4*>(p));
+  const T* x = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) v[i] = load_f32(x + i);
+}
+
+// The share of k of this CTA, and its rows.
+__device__ __forceinline__ void share(const Thin& t, long long unit, long long* k0, long long* k1) {
+  const long long units = (t.nk + unit - 1) / unit, r = t.splits > 1 ? blockIdx.x % t.splits : 0;
+  *k0 = units * r / t.splits * unit;
+  *k1 = min(t.nk, units * (r + 1) / t.splits * unit);
+}
+
+// S[s][k0 .. k0 + n) -> shared memory, [k][kT] or [kT][n], noughts behind the last row.
+template <typename T, int kT, bool kByK>
+__device__ __forceinline__ void stage_short(const Thin& t, long long k0, int n, float* sh, int pitch) {
+  for (int i = threadIdx.x; i < n * kT; i += kThreads) {
+    const int s = t.S.ks == 1 ? i / n : i % kT, k = t.S.ks == 1 ? i % n : i / kT;
+    const float v = s < t.ns ? load_f32(static_cast<const T*>(t.S.p) + s * t.S.rs + (k0 + k) * t.S.ks) : 0.f;
+    sh[kByK ? k * kT + s : s * pitch + k] = v;
+  }
+}
+
+template <typename T, int kT, int kR>
+__global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thin t) {
+  constexpr int kV = 16 / sizeof(T), kStage = kStageFloats / kT;
+  __shared__ __align__(16) float sh[kStageFloats];
+  __shared__ float red[kWarps][kR * kT];
+  __shared__ float sum[kWarps][kR * kT];
+  chain_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long group = (long long)(blockIdx.x / t.splits);
+  const long long l0 = t.wk == 1 ? (group * kWarps + warp) * kR : group * kR;
+  long long k0, k1;
+  share(t, kStage < 1024 ? kStage : 1024, &k0, &k1);
+  float acc[kR][kT] = {};
+  const T* row[kR];
+#pragma unroll
+  for (int r = 0; r < kR; ++r) row[r] = static_cast<const T*>(t.L.p) + min(l0 + r, t.nl - 1) * t.L.rs;
+  for (long long kb = k0; kb < k1; kb += kStage) {
+    const int n = (int)min((long long)kStage, k1 - kb);
+    __syncthreads();
+    stage_short<T, kT, false>(t, kb, n, sh, kStage);
+    __syncthreads();
+    const int at = t.wk == 1 ? lane : warp * 32 + lane, step = t.wk == 1 ? 32 : 256;
+    if (t.vec) {
+      const int groups = n / kV;
+#pragma unroll 4
+      for (int i = at; i < groups; i += step) {
+        float x[kR][kV];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) load_vec(row[r] + kb + (long long)i * kV, x[r]);
+#pragma unroll
+        for (int s = 0; s < kT; ++s) {
+          float y[kV];
+#pragma unroll
+          for (int v = 0; v < kV; v += 4) *reinterpret_cast<float4*>(y + v) = *reinterpret_cast<const float4*>(sh + s * kStage + i * kV + v);
+#pragma unroll
+          for (int r = 0; r < kR; ++r)
+#pragma unroll
+            for (int v = 0; v < kV; ++v) acc[r][s] = fmaf(x[r][v], y[v], acc[r][s]);
+        }
+      }
+    }
+    for (int k = (t.vec ? n / kV * kV : 0) + at; k < n; k += step) {
+#pragma unroll
+      for (int r = 0; r < kR; ++r) {
+        const float x = load_f32(row[r] + (kb + k) * t.L.ks);
+#pragma unroll
+        for (int s = 0; s < kT; ++s) acc[r][s] = fmaf(x, sh[s * kStage + k], acc[r][s]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+#pragma unroll
+    for (int s = 0; s < kT; ++s) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) acc[r][s] += __shfl_xor_sync(0xffffffffu, acc[r][s], o);
+      if (lane == 0) red[warp][r * kT + s] = acc[r][s];
+    }
+  // sums of the CTA: one set per warp, or one for all of them
+  __syncthreads();
+  const int sets = t.wk == 1 ? kWarps : 1;
+  for (int i = threadIdx.x; i < sets * kR * kT; i += kThreads) {
+    const int w = i / (kR * kT), e = i % (kR * kT);
+    float v = red[w][e];
+    if (t.wk != 1) for (int u = 1; u < kWarps; ++u) v += red[u][e];
+    sum[w][e] = v;
+  }
+  if (t.splits > 1) cluster_sync(); else __syncthreads();
+  if (t.splits == 1 || blockIdx.x % t.splits == 0) {
+    for (int i = threadIdx.x; i < sets * kR * kT; i += kThreads) {
+      const int w = i / (kR * kT), e = i % (kR * kT), s = e % kT;
+      const long long l = (t.wk == 1 ? (group * kWarps + w) * kR : group * kR) + e / kT;
+      if (l >= t.nl || s >= t.ns) continue;
+      float v = sum[w][e];
+      for (int p = 1; p < t.splits; ++p) v += load_peer(&sum[w][e], (uint32_t)p);
+      finish_thin<T>(t, v, l, s);
+    }
+  }
+  if (t.splits > 1) cluster_sync();                      // nobody leaves while its sums may be read
+}
+
+template <typename T, int kT>
+__global__ void __launch_bounds__(kThreads) k_thin_rows(const __grid_constant__ Thin t) {
+  constexpr int kV = 16 / sizeof(T), kTile = 32 * kV, kStage = kStageFloats / kT;
+  __shared__ __align__(16) float sh[kStageFloats];
+  float* sum = sh;                                       // [kT][kTile], when the last of the short side has been used
+  static_assert(kT * kTile <= kStageFloats, "the sums take the stage's place");
+  chain_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long l0 = (long long)(blockIdx.x / t.splits) * kTile, l = l0 + lane * kV;
+  long long k0, k1;
+  share(t, 64, &k0, &k1);
+  const bool whole = t.vec && l + kV <= t.nl;
+  float acc[kT][kV] = {};
+  for (long long kb = k0; kb < k1; kb += kStage) {
+    const int n = (int)min((long long)kStage, k1 - kb);
+    __syncthreads();
+    stage_short<T, kT, true>(t, kb, n, sh, 0);
+    __syncthreads();
+    const T* at = static_cast<const T*>(t.L.p) + kb * t.L.ks + l * t.L.rs;
+#pragma unroll 4
+    for (int k = warp; k < n; k += kWarps) {
+      float x[kV];
+      if (whole) {
+        load_vec(at + k * t.L.ks, x);
+      } else {
+#pragma unroll
+        for (int v = 0; v < kV; ++v) x[v] = l + v < t.nl ? load_f32(at + k * t.L.ks + v * t.L.rs) : 0.f;
+      }
+      float y[kT];
+#pragma unroll
+      for (int s = 0; s < kT; ++s) y[s] = sh[k * kT + s];
+#pragma unroll
+      for (int s = 0; s < kT; ++s)
+#pragma unroll
+        for (int v = 0; v < kV; ++v) acc[s][v] = fmaf(x[v], y[s], acc[s][v]);
+    }
+  }
+  for (int w = 0; w < kWarps; ++w) {                     // in the order of the warps
+    __syncthreads();
+    if (warp == w)
+#pragma unroll
+      for (int s = 0; s < kT; ++s)
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+          float* p = sum + s * kTile + v * 32 + lane;      // (a lane's rows 32 apart: no bank conflicts)
+          *p = w == 0 ? acc[s][v] : *p + acc[s][v];
+        }
+  }
+  if (t.splits > 1) cluster_sync(); else __syncthreads();
+  const int rank = t.splits > 1 ? (int)(blockIdx.x % t.splits) : 0;
+  for (int i = rank * kThreads + threadIdx.x; i < kT * kTile; i += kThreads * t.splits) {
+    const int s = i / kTile, j = i % kTile;              // row j of the tile is lane j / kV's, its (j % kV)-th
+    if (l0 + j >= t.nl || s >= t.ns) continue;
+    const float* p = sum + s * kTile + (j % kV) * 32 + j / kV;
+    float v = 0.f;
+    if (t.splits == 1) v = *p;
+    else for (int q = 0; q < t.splits; ++q) v += load_peer(p, (uint32_t)q);
+    finish_thin<T>(t, v, l0 + j, s);
+  }
+  if (t.splits > 1) cluster_sync();
+}
+
+bool vec_ok(const void* p, long long pitch, size_t size) { return ((uintptr_t)p & 15) == 0 && (pitch * size) % 16 == 0; }
+
+template <typename T, int kT>
+cudaError_t launch(Thin t, int sms, cudaStream_t s) {
+  const bool along_k = t.L.ks == 1 || t.L.rs != 1;
+  if (along_k) {
+    t.vec = t.L.ks == 1 && (t.nl == 1 || vec_ok(t.L.p, t.L.rs, sizeof(T))) && ((uintptr_t)t.L.p & 15) == 0;
+    constexpr int kR = kT >= 4 ? 2 : 1;
+    const long long warps = (t.nl + kR - 1) / kR;
+    t.wk = warps >= 4 * sms ? 1 : kWarps;                // few rows: the warps of a CTA share them
+    const long long groups = t.wk == 1 ? (warps + kWarps - 1) / kWarps : warps;
+    t.splits = 1;
+    while (t.splits < 8 && groups * t.splits * 2 <= 2 * sms && t.nk >= 4096ll * t.splits) t.splits *= 2;
+    return launch_chained_cluster(k_thin_k<T, kT, kR>, dim3((unsigned)(groups * t.splits)), kThreads, 0, s, t.splits, t);
+  }
+  t.vec = vec_ok(t.L.p, t.L.ks, sizeof(T));
+  const long long tiles = (t.nl + 32 * (16 / sizeof(T)) - 1) / (32 * (16 / sizeof(T)));
+  t.splits = 1;
+  while (t.splits < 8 && tiles * t.splits * 2 <= 4 * sms && t.nk >= 256ll * t.splits) t.splits *= 2;
+  return launch_chained_cluster(k_thin_rows<T, kT>, dim3((unsigned)(tiles * t.splits)), kThreads, 0, s, t.splits, t);
+}
+template <typename T>
+cudaError_t by_short(const Thin& t, int sms, cudaStream_t s) {
+  return t.ns == 1 ? launch<T, 1>(t, sms, s) : t.ns == 2 ? launch<T, 2>(t, sms, s) : t.ns <= 4 ? launch<T, 4>(t, sms, s) : launch<T, 8>(t, sms, s);
+}
+
+}  // namespace
+
+cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  Thin t = {};
+  t.f = f; t.nk = nk;
+  t.swapped = na < nb;
+  t.L = t.swapped ? B : A; t.S = t.swapped ? A : B;
+  t.nl = t.swapped ? nb : na; t.ns = (int)(t.swapped ? na : nb);
+  return type == STRADS_F32 ? by_short<float>(t, sms, s) : type == STRADS_BF16 ? by_short<__nv_bfloat16>(t, sms, s) : by_short<__half>(t, sms, s);
+}
+
+}  // namespace strads

@@ -305,6 +305,19 @@ def test_gradients_against_differences(b):
             assert abs((f[0] - f[1]) * 32 - float(terms.sum())) <= 1e-3 * float(terms.abs().sum())
 
 
+def test_a_wait_that_runs_out_is_reported(b):
+    """Operand loads withheld: the call ends after milliseconds, the status says so once, and the next call is right."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, w = matrix(300, 512, torch.bfloat16, gen), matrix(256, 512, torch.bfloat16, gen)
+    assert b.linear_status() == (0, 0)
+    want = b.linear_forward(x, w)
+    b.linear_forward(x, w, flags=b.LINEAR_FLAG_STALL)
+    assert b.linear_status() == (-6, 4)
+    assert b.linear_status() == (0, 0)
+    assert torch.equal(b.linear_forward(x, w), want)
+    assert b.linear_status() == (0, 0)
+
+
 def test_the_binding_refuses(b):
     x, w = torch.zeros(4, 8, device="cuda"), torch.zeros(3, 8, device="cuda")
     for call in (lambda: b.linear_forward(x, w[:, :7]), lambda: b.linear_forward(x, w.cpu()), lambda: b.linear_forward(x, w, bias=torch.zeros(4, device="cuda")),
