@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 
+import numpy as np
 import torch
 
 from . import workloads as wl
@@ -17,6 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libstrads_b200.so")
 
 OK = 0
+ERR_WORKSPACE_TOO_SMALL = -3
 FLAG_UNIFORM_DRAW = 1
 FLAG_NO_FILTER = 2
 FLAG_SIMT_GRAM = 4
@@ -80,7 +82,8 @@ class Matrix(C.Structure):
 
 class LinearConfig(C.Structure):
     _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("n_rows", C.c_int64), ("n_in", C.c_int64), ("n_out", C.c_int64),
-                ("x", Matrix), ("w", Matrix), ("scale", C.c_float), ("flags", C.c_uint32), ("workspace", C.c_void_p),
+                ("x", C.c_void_p), ("x_row_stride", C.c_int64), ("x_col_stride", C.c_int64),
+                ("w", C.c_void_p), ("w_row_stride", C.c_int64), ("w_col_stride", C.c_int64), ("scale", C.c_float), ("flags", C.c_uint32), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
@@ -347,70 +350,86 @@ class StradsLasso:
             pass
 
 
-def _matrix(t, what, like, shape):
+def _refuse(t, what, dtype, index, shape):
+    if t.dtype != dtype:
+        raise TypeError(f"{what} of type {t.dtype}, {dtype} expected")
+    if t.get_device() != index:
+        raise ValueError(f"{what} on {t.device}, cuda:{index} expected")
+    raise ValueError(f"{what} must be {'contiguous, ' if len(shape) == 1 else ''}of shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+def _matrix(t, what, dtype, index, shape):
     """A tensor as the library takes it; refuses other types, devices and shapes than those of the call."""
-    if t.dtype != like.dtype:
-        raise TypeError(f"{what} of type {t.dtype}, {like.dtype} expected")
-    if t.device != like.device:
-        raise ValueError(f"{what} on {t.device}, {like.device} expected")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what} of shape {tuple(t.shape)}, {tuple(shape)} expected")
-    return Matrix(t.data_ptr(), t.stride(0), t.stride(1))
+    if t.dtype != dtype or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, dtype, index, shape)
+    rs, cs = t.stride()
+    return Matrix(t.data_ptr(), rs, cs)
+
+
+def _vector(t, what, dtype, index, n):
+    if t.dtype != dtype or t.get_device() != index or t.shape != (n,) or not t.is_contiguous():
+        _refuse(t, what, dtype, index, (n,))
+    return t.data_ptr()
 
 
 def _linear_config(x, w, activation, scale, flags):
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x and w must have two dimensions")
-    if x.device.type != "cuda":
+    index, dtype = x.get_device(), x.dtype
+    if index < 0:
         raise ValueError("x must live on a CUDA device")
-    if x.dtype not in TYPES:
-        raise TypeError(f"x of type {x.dtype}")
+    if dtype not in TYPES:
+        raise TypeError(f"x of type {dtype}")
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
-    (n, k), m = x.shape, w.shape[0]
-    cfg = LinearConfig(type=TYPES[x.dtype], activation=ACTIVATIONS[activation], n_rows=n, n_in=k, n_out=m, scale=scale, flags=flags)
-    cfg.x, cfg.w = _matrix(x, "x", x, (n, k)), _matrix(w, "w", x, (m, k))
-    return cfg
+    n, k = x.shape
+    m = w.shape[0]
+    if w.dtype != dtype or w.get_device() != index or w.shape[1] != k:
+        _refuse(w, "w", dtype, index, (m, k))
+    xr, xc = x.stride()
+    wr, wc = w.stride()
+    cfg = LinearConfig(TYPES[dtype], ACTIVATIONS[activation], n, k, m, x.data_ptr(), xr, xc, w.data_ptr(), wr, wc, scale, flags, None, 0,
+                       torch._C._cuda_getCurrentRawStream(index))
+    return cfg, n, k, m, dtype, index
 
 
-def _linear_workspace(cfg, which, device):
-    """The call's workspace: from the caching allocator, on the current stream, so that no two calls share one unless they follow each other."""
-    need = (C.c_size_t * 2)()
-    _check(load().strads_linear_workspace_bytes(C.byref(cfg), C.cast(C.byref(need, 0), C.POINTER(C.c_size_t)),
-                                                C.cast(C.byref(need, C.sizeof(C.c_size_t)), C.POINTER(C.c_size_t))), "strads_linear_workspace_bytes")
-    ws = torch.empty(need[which], dtype=torch.uint8, device=device) if need[which] else None
-    cfg.workspace, cfg.workspace_bytes = (ws.data_ptr() if ws is not None else None), need[which]
-    cfg.stream = torch.cuda.current_stream().cuda_stream
-    return ws
-
-
-def _vector(t, what, like, n):
-    if t.dtype != like.dtype:
-        raise TypeError(f"{what} of type {t.dtype}, {like.dtype} expected")
-    if t.device != like.device or tuple(t.shape) != (n,) or not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous, of shape ({n},) and on {like.device}")
-    return C.c_void_p(t.data_ptr())
+def _linear_call(call, where, cfg, which, device):
+    """The call with no workspace, and where it needs one with one from the caching allocator, on the current stream, so that two
+    calls only share one where they follow each other."""
+    rc = call()
+    if rc == ERR_WORKSPACE_TOO_SMALL:
+        need = (C.c_size_t(0), C.c_size_t(0))
+        _check(load().strads_linear_workspace_bytes(C.byref(cfg), C.byref(need[0]), C.byref(need[1])), "strads_linear_workspace_bytes")
+        ws = torch.empty(need[which].value, dtype=torch.uint8, device=device)
+        cfg.workspace, cfg.workspace_bytes = ws.data_ptr(), need[which].value
+        rc = call()
+    if rc != OK:
+        _check(rc, where)
 
 
 def linear_forward(x, w, bias=None, residual=None, activation="identity", scale=1.0, want_preact=False, out=None, preact=None, flags=0):
     """out = residual + scale * activation(x w^T + bias) (strads_linear_forward).  x [n_rows, n_in] and w [n_out, n_in] in either
     order, float32, bfloat16 or float16; residual [n_rows, n_out] may be an expanded tensor, and out may be the residual itself.
     Returns out, and with want_preact (or preact, a tensor for it) the pair (out, x w^T + bias)."""
-    cfg = _linear_config(x, w, activation, scale, flags)
-    shape = (cfg.n_rows, cfg.n_out)
-    b = None if bias is None else _vector(bias, "bias", x, cfg.n_out)
-    r = None if residual is None else C.byref(_matrix(residual, "residual", x, shape))
-    with torch.cuda.device(x.device):
-        if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=x.device)
-        if preact is None and want_preact:
-            preact = torch.empty(shape, dtype=x.dtype, device=x.device)
-        o = _matrix(out, "out", x, shape)
-        z = None if preact is None else C.byref(_matrix(preact, "preact", x, shape))
-        ws = _linear_workspace(cfg, 0, x.device)
-        _check(load().strads_linear_forward(C.byref(cfg), b, r, C.byref(o), z), "strads_linear_forward")
-    del ws
+    cfg, n, _, m, dtype, index = _linear_config(x, w, activation, scale, flags)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return linear_forward(x, w, bias, residual, activation, scale, want_preact, out, preact, flags)
+    lib, shape = load(), (n, m)
+    b = None if bias is None else _vector(bias, "bias", dtype, index, m)
+    r = None if residual is None else C.byref(_matrix(residual, "residual", dtype, index, shape))
+    if out is None:
+        out = x.new_empty(shape)
+    if preact is None and want_preact:
+        preact = x.new_empty(shape)
+    o = C.byref(_matrix(out, "out", dtype, index, shape))
+    z = None if preact is None else C.byref(_matrix(preact, "preact", dtype, index, shape))
+    _linear_call(lambda: lib.strads_linear_forward(C.byref(cfg), b, r, o, z), "strads_linear_forward", cfg, 0, x.device)
     return out if preact is None else (out, preact)
+
+
+def _empty_in_order_of(t):
+    return t.new_empty(t.shape[::-1]).t() if t.stride(0) < t.stride(1) else t.new_empty(t.shape)
 
 
 def linear_backward(grad_out, x, w, preact=None, activation="identity", scale=1.0, want_x=True, want_w=True, want_bias=True,
@@ -418,27 +437,25 @@ def linear_backward(grad_out, x, w, preact=None, activation="identity", scale=1.
     """Gradients of linear_forward (strads_linear_backward) from grad_out [n_rows, n_out] and the preact that the forward pass gave
     (not with the identity): (grad_x, grad_w, grad_bias), None where not wanted.  New gradients have the order of x and w.  The residual's
     gradient is grad_out itself."""
-    cfg = _linear_config(x, w, activation, scale, flags)
-    shape = (cfg.n_rows, cfg.n_out)
-    g = _matrix(grad_out, "grad_out", x, shape)
-    if activation != "identity" and preact is None:
+    cfg, n, k, m, dtype, index = _linear_config(x, w, activation, scale, flags)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return linear_backward(grad_out, x, w, preact, activation, scale, want_x, want_w, want_bias, grad_x, grad_w, grad_bias, flags)
+    lib, shape = load(), (n, m)
+    g = C.byref(_matrix(grad_out, "grad_out", dtype, index, shape))
+    if preact is None and activation != "identity":
         raise ValueError("the gradient needs preact")
-    z = None if preact is None else C.byref(_matrix(preact, "preact", x, shape))
-    like = lambda t: torch.empty(t.shape[::-1], dtype=t.dtype, device=t.device).t() if t.stride(0) < t.stride(1) else \
-        torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    with torch.cuda.device(x.device):
-        if want_x and grad_x is None:
-            grad_x = like(x)
-        if want_w and grad_w is None:
-            grad_w = like(w)
-        if want_bias and grad_bias is None:
-            grad_bias = torch.empty(cfg.n_out, dtype=x.dtype, device=x.device)
-        gx = None if grad_x is None else C.byref(_matrix(grad_x, "grad_x", x, x.shape))
-        gw = None if grad_w is None else C.byref(_matrix(grad_w, "grad_w", x, w.shape))
-        gb = None if grad_bias is None else _vector(grad_bias, "grad_bias", x, cfg.n_out)
-        ws = _linear_workspace(cfg, 1, x.device)
-        _check(load().strads_linear_backward(C.byref(cfg), C.byref(g), z, gx, gw, gb), "strads_linear_backward")
-    del ws
+    z = None if preact is None else C.byref(_matrix(preact, "preact", dtype, index, shape))
+    if want_x and grad_x is None:
+        grad_x = _empty_in_order_of(x)
+    if want_w and grad_w is None:
+        grad_w = _empty_in_order_of(w)
+    if want_bias and grad_bias is None:
+        grad_bias = x.new_empty(m)
+    gx = None if grad_x is None else C.byref(_matrix(grad_x, "grad_x", dtype, index, (n, k)))
+    gw = None if grad_w is None else C.byref(_matrix(grad_w, "grad_w", dtype, index, (m, k)))
+    gb = None if grad_bias is None else _vector(grad_bias, "grad_bias", dtype, index, m)
+    _linear_call(lambda: lib.strads_linear_backward(C.byref(cfg), g, z, gx, gw, gb), "strads_linear_backward", cfg, 1, x.device)
     return grad_x, grad_w, grad_bias
 
 
@@ -498,6 +515,8 @@ class AdamW:
         self._cfg = AdamWConfig(param_type=TYPES[dtype], state_bits=bits, beta1=betas[0], beta2=betas[1], eps=eps,
                                 weight_decay=weight_decay, l1=l1)
         self._list = (AdamWTensor * len(params))()
+        self._grads = np.frombuffer(self._list, dtype=np.uint64).reshape(len(params), -1)[:, AdamWTensor.grad.offset // 8]
+        self._sizes, self._index = sizes, dev.index
         for i, p in enumerate(params):
             e = self._list[i]
             e.param, e.n = p.data_ptr(), p.numel()
@@ -537,9 +556,14 @@ class AdamW:
         step runs: a captured step then follows them; skip other than 0 leaves everything as it is."""
         grads = list(grads)
         gtype = grads[0].dtype if grads else None
-        if gtype not in (torch.float32, self.dtype):
+        if gtype is not torch.float32 and gtype is not self.dtype:
             raise TypeError(f"gradients of type {gtype}")
-        self._check("gradients", grads, gtype, [p.numel() for p in self.params])
+        if ([g.numel() for g in grads] != self._sizes or {g.dtype for g in grads} != {gtype} or
+                {g.get_device() for g in grads} != {self._index} or not all([g.is_contiguous() for g in grads])):
+            self._check("gradients", grads, gtype, self._sizes)
+        if self._index != torch._C._cuda_getDevice():
+            with torch.cuda.device(self._index):
+                return self.step(grads, lr, step, grad_scale, skip)
         c, on_device = self._cfg, lambda t: isinstance(t, torch.Tensor)
         c.grad_type = TYPES[gtype]
         c.lr_dev = self._scalar(lr, torch.float32) if on_device(lr) else None
@@ -547,11 +571,11 @@ class AdamW:
         c.grad_scale_dev = self._scalar(grad_scale, torch.float32) if on_device(grad_scale) else None
         c.skip_dev = self._scalar(skip, torch.int32)
         c.lr, c.grad_scale, c.step = 0.0 if on_device(lr) else lr, 1.0 if on_device(grad_scale) else grad_scale, 1 if on_device(step) else step
-        for e, g in zip(self._list, grads):
-            e.grad = g.data_ptr()
-        with torch.cuda.device(self.device):
-            c.stream = torch.cuda.current_stream().cuda_stream
-            _check(load().strads_adamw_step(C.byref(c), self._list, len(grads)), "strads_adamw_step")
+        self._grads[:] = [g.data_ptr() for g in grads]
+        c.stream = torch._C._cuda_getCurrentRawStream(self._index)
+        rc = load().strads_adamw_step(C.byref(c), self._list, len(grads))
+        if rc != OK:
+            _check(rc, "strads_adamw_step")
 
     def moments(self, out=None):
         """(first, second): the moments as lists of float32 tensors.  32 bits: the state itself.  8 bits: the values that the

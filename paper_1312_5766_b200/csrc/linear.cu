@@ -12,8 +12,7 @@ __device__ unsigned int g_linear_status;       // STRADS_STATUS_* bits of the la
 constexpr int kThreads = 256;
 
 // ---- operands of the tensor-core products that cannot be read in place ----
-// dst[plane][outer][ld] from src, eight neighbours per thread.  binary32: x = p0 + p1 + p2, each the nearest bfloat16 to what is left
-// (24 bits together; where the nearest would be infinite, the next towards 0); what is not finite stays in p0 alone.
+// dst[plane][outer][ld] from src, eight neighbours per thread; binary32 as three planes of bfloat16 (split_pair).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long long outer_stride, long long inner_stride, long long outer, long long inner,
                                                           unsigned short* dst, long long ld, long long plane, int vec) {
@@ -36,17 +35,12 @@ __global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long lon
     if (sizeof(T) == 2) {
       *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
     } else {
-      __align__(16) __nv_bfloat16 p[3][8];
+      __align__(16) uint32_t p[3][4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = load_f32(&x[j]);
-        const bool finite = fabsf(v) <= 3.402823466e38f;
-        float h = __bfloat162float(__float2bfloat16_rn(v));
-        if (finite && fabsf(h) > 3.402823466e38f) h = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-        const float r1 = finite ? v - h : 0.f, m = __bfloat162float(__float2bfloat16_rn(r1));
-        p[0][j] = __float2bfloat16_rn(h);
-        p[1][j] = __float2bfloat16_rn(r1);
-        p[2][j] = __float2bfloat16_rn(r1 - m);
+      for (int j = 0; j < 4; ++j) {
+        uint32_t w[3];
+        split_pair(load_f32(&x[2 * j]), load_f32(&x[2 * j + 1]), w);
+        p[0][j] = w[0]; p[1][j] = w[1]; p[2][j] = w[2];
       }
 #pragma unroll
       for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + q * plane) = *reinterpret_cast<const uint4*>(p[q]);
@@ -86,12 +80,17 @@ __global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand pr
       }
     }
     __align__(16) T out[8];
+    float v[8], zf[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float v = scale * load_f32(&g[j]);
-      if (act != STRADS_ACT_IDENTITY) v *= slope(load_f32(&z[j]), act);
-      total[j] += v;
-      store_f32(&out[j], v);
+      v[j] = scale * load_f32(&g[j]);
+      zf[j] = act != STRADS_ACT_IDENTITY ? load_f32(&z[j]) : 0.f;
+    }
+    times_slope<sizeof(T) == 4>(zf, v, act);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      total[j] += v[j];
+      store_f32(&out[j], v[j]);
     }
     if (gz != nullptr && c < m) {                        // (ld is a multiple of 8: the last group has its place)
 #pragma unroll
@@ -187,12 +186,13 @@ struct Matrix {
   Operand m;                             // element (row, column)
   long long rows, cols;
   bool unknown, brought;
+  int order;                             // which of two equally long sides counts as the longer: the same whichever way D lies
   Planes p;
 };
 Operand operand_of(const strads_const_matrix_t& m) { return Operand{m.data, (long long)m.row_stride, (long long)m.col_stride}; }
-Matrix matrix_of(const Operand& m, long long rows, long long cols) {
+Matrix matrix_of(const Operand& m, long long rows, long long cols, int order) {
   Matrix x = {};
-  x.m = m; x.rows = rows; x.cols = cols;
+  x.m = m; x.rows = rows; x.cols = cols; x.order = order;
   return x;
 }
 Planes side_of(Call& c, Matrix& x, bool columns_as_rows) {
@@ -210,6 +210,17 @@ void product(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
     if (c.run && c.err == cudaSuccess) c.err = launch_linear_thin(c.type, a, b, na, nb, nk, f, c.stream);
     return;
   }
+  // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 64
+  // rows, where planes in memory cost 16)
+  const bool b_long = na < nb || (na == nb && B.order < A.order);
+  const Operand& l = b_long ? b : a;
+  if (c.size == 4 && (b_long ? na : nb) <= kSplitMost && (l.rs == 1 || l.ks == 1)) {
+    const long long nl = b_long ? nb : na, ns = b_long ? na : nb;
+    const Planes p = b_long ? side_of(c, A, ta) : side_of(c, B, tb);
+    void* ws = c.take(linear_split_workspace(nl, ns, nk));
+    if (c.run && c.err == cudaSuccess) c.err = launch_linear_split(l, p, nl, ns, nk, b_long, f, ws, c.status, c.stall, c.stream);
+    return;
+  }
   const Planes pa = side_of(c, A, ta), pb = side_of(c, B, tb);
   if (c.run && c.err == cudaSuccess) c.err = launch_linear_tc(c.type, pa, pb, na, nb, nk, f, c.status, c.stall, c.stream);
 }
@@ -220,7 +231,7 @@ bool rows_run(long long rs, long long cs) { return cs != 1 && rs == 1; }
 
 void forward(Call& c, const strads_linear_config_t& g, const void* bias, const strads_const_matrix_t* residual, const strads_matrix_t* out,
              const strads_matrix_t* preact) {
-  Matrix x = matrix_of(operand_of(g.x), g.n_rows, g.n_in), w = matrix_of(operand_of(g.w), g.n_out, g.n_in);
+  Matrix x = matrix_of(operand_of(g.x), g.n_rows, g.n_in, 0), w = matrix_of(operand_of(g.w), g.n_out, g.n_in, 1);
   Finish f = {};
   f.act = g.activation; f.scale = g.scale; f.bias = bias;
   bool ar = false;
@@ -271,7 +282,7 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
   if (formed || gbias != nullptr || !c.run) gradient_of_z<T>(c, g, gout, preact, gz, ld, static_cast<T*>(gbias));
   Operand kept = operand_of(gout);
   if (formed) { kept.p = gz; kept.rs = ld; kept.ks = 1; }
-  Matrix z = matrix_of(kept, g.n_rows, g.n_out), x = matrix_of(operand_of(g.x), g.n_rows, g.n_in), w = matrix_of(operand_of(g.w), g.n_out, g.n_in);
+  Matrix z = matrix_of(kept, g.n_rows, g.n_out, 2), x = matrix_of(operand_of(g.x), g.n_rows, g.n_in, 0), w = matrix_of(operand_of(g.w), g.n_out, g.n_in, 1);
   z.unknown = !formed && !c.run;
   Finish f = {};
   f.plain = 1;
@@ -358,8 +369,8 @@ static int check_workspace(const strads_linear_config_t& c, int which) {
   const int rc = strads_linear_workspace_bytes(&c, &need[0], &need[1]);
   if (rc != STRADS_OK) return rc;
   if (need[which] == 0) return STRADS_OK;
-  if (c.workspace == nullptr || ((uintptr_t)c.workspace & 255) != 0) return STRADS_ERR_INVALID_ARG;
-  return c.workspace_bytes < need[which] ? STRADS_ERR_WORKSPACE_TOO_SMALL : STRADS_OK;
+  if (c.workspace_bytes < need[which]) return STRADS_ERR_WORKSPACE_TOO_SMALL;
+  return c.workspace == nullptr || ((uintptr_t)c.workspace & 255) != 0 ? STRADS_ERR_INVALID_ARG : STRADS_OK;
 }
 
 int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, const strads_const_matrix_t* residual,

@@ -28,52 +28,96 @@ __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_f32(__half* p, float v) { *p = __float2half_rn(v); }
 
-// 1/2 z (1 + tanh u) = z sigma(2u), u = sqrt(2/pi) (z + 0.044715 z^3): in this form nothing cancels for negative z.
-__device__ __forceinline__ float tanh_argument2(float z) { return 1.5957691216057308f * (z + 0.044715f * z * z * z); }
-__device__ __forceinline__ float sigmoid_f32(float z) { return 1.f / (1.f + expf(-z)); }
-__device__ __forceinline__ float activate(float z, int act) {
-  switch (act) {
-    case STRADS_ACT_RELU: return z < 0.f ? 0.f : z;                    // (a NaN stays one)
-    case STRADS_ACT_SIGMOID: return sigmoid_f32(z);
-    case STRADS_ACT_GELU: return z * normcdff(z);
-    case STRADS_ACT_GELU_TANH: return z * sigmoid_f32(tanh_argument2(z));
-    case STRADS_ACT_SILU: return z * sigmoid_f32(z);
-    default: return z;
-  }
+// Functions for binary32 results (kExact) by CUDA's own, for 16-bit ones to 2^-20: the hardware's exponential and quotient, and
+// Phi(-z), z >= 0, as exp(-z^2/2) t P(t), t = 1 / (1 + 0.285 z): P is fitted to erfcx, weighted so that the relative error is even
+// (1.6e-7; 4.7e-7 as evaluated here).  Nothing cancels for negative z in any of them.
+template <bool kExact>
+__device__ __forceinline__ float sigmoid_f32(float z) { return kExact ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float normal_tail(float a, float e) {      // Phi(-a), e = exp(-a^2/2)
+  const float t = __fdividef(1.f, fmaf(0.285f, a, 1.f));
+  float p = 0.024569256f;
+  p = fmaf(p, t, -0.08659119f);
+  p = fmaf(p, t, 0.07391585f);
+  p = fmaf(p, t, 0.003500571f);
+  p = fmaf(p, t, 0.06757765f);
+  p = fmaf(p, t, 0.08512555f);
+  p = fmaf(p, t, 0.10450529f);
+  p = fmaf(p, t, 0.11369858f);
+  p = fmaf(p, t, 0.11369853f);
+  return p * t * e;
 }
-__device__ __forceinline__ float slope(float z, int act) {
-  switch (act) {
-    case STRADS_ACT_RELU: return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    case STRADS_ACT_SIGMOID: { const float s = sigmoid_f32(z); return s * sigmoid_f32(-z); }
-    case STRADS_ACT_GELU: return normcdff(z) + z * expf(-0.5f * z * z) * 0.3989422804014327f;
-    case STRADS_ACT_GELU_TANH: {
-      const float u = tanh_argument2(z), s = sigmoid_f32(u), near = fminf(fmaxf(z, -40.f), 40.f);      // (beyond, the second term is 0)
-      return s + z * s * sigmoid_f32(-u) * 1.5957691216057308f * (1.f + 0.134145f * near * near);
-    }
-    case STRADS_ACT_SILU: { const float s = sigmoid_f32(z); return s * (1.f + z * sigmoid_f32(-z)); }
-    default: return 1.f;
+// 1/2 z (1 + tanh u) = z sigma(2u), u = sqrt(2/pi) (z + 0.044715 z^3).
+__device__ __forceinline__ float tanh_argument2(float z) { return 1.5957691216057308f * z * fmaf(0.044715f * z, z, 1.f); }
+
+template <bool kExact, int kAct>
+__device__ __forceinline__ float activate_as(float z) {
+  if (kAct == STRADS_ACT_RELU) return z < 0.f ? 0.f : z;               // (a NaN stays one)
+  if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z);
+  if (kAct == STRADS_ACT_GELU) {
+    if (kExact) return z * normcdff(z);
+    const float q = z * normal_tail(fabsf(z), __expf(-0.5f * z * z));
+    return z > 0.f ? z - q : q;
   }
+  if (kAct == STRADS_ACT_GELU_TANH) return z * sigmoid_f32<kExact>(tanh_argument2(z));
+  if (kAct == STRADS_ACT_SILU) return z * sigmoid_f32<kExact>(z);
+  return z;
+}
+template <bool kExact, int kAct>
+__device__ __forceinline__ float slope_as(float z) {
+  if (kAct == STRADS_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+  if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z) * sigmoid_f32<kExact>(-z);
+  if (kAct == STRADS_ACT_GELU) {
+    const float e = kExact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
+    const float near = fminf(fmaxf(z, -40.f), 40.f);                   // (beyond, e is 0)
+    float phi;
+    if (kExact) {
+      phi = normcdff(z);
+    } else {
+      const float q = normal_tail(fabsf(z), e);
+      phi = z > 0.f ? 1.f - q : q;
+    }
+    return fmaf(near * 0.3989422804014327f, e, phi);
+  }
+  if (kAct == STRADS_ACT_GELU_TANH) {
+    const float u = tanh_argument2(z), near = fminf(fmaxf(z, -40.f), 40.f);      // (beyond, the second term is 0)
+    const float s = sigmoid_f32<kExact>(u), o = sigmoid_f32<kExact>(-u);
+    return fmaf(near * s * o, 1.5957691216057308f * fmaf(0.134145f * near, near, 1.f), s);
+  }
+  if (kAct == STRADS_ACT_SILU) return sigmoid_f32<kExact>(z) * fmaf(z, sigmoid_f32<kExact>(-z), 1.f);
+  return 1.f;
 }
 
-// The same for several values: one branch for all of them.
-template <int kN>
+// Several values: one branch for all of them.
+template <bool kExact, int kAct, int kN>
+__device__ __forceinline__ void activate_run(float (&v)[kN]) {
+#pragma unroll
+  for (int j = 0; j < kN; ++j) v[j] = activate_as<kExact, kAct>(v[j]);
+}
+template <bool kExact, int kN>
 __device__ __forceinline__ void activate_all(float (&v)[kN], int act) {
-  if (act == STRADS_ACT_IDENTITY) return;
-  if (act == STRADS_ACT_RELU) {
+  switch (act) {
+    case STRADS_ACT_RELU: activate_run<kExact, STRADS_ACT_RELU>(v); break;
+    case STRADS_ACT_SIGMOID: activate_run<kExact, STRADS_ACT_SIGMOID>(v); break;
+    case STRADS_ACT_GELU: activate_run<kExact, STRADS_ACT_GELU>(v); break;
+    case STRADS_ACT_GELU_TANH: activate_run<kExact, STRADS_ACT_GELU_TANH>(v); break;
+    case STRADS_ACT_SILU: activate_run<kExact, STRADS_ACT_SILU>(v); break;
+    default: break;
+  }
+}
+template <bool kExact, int kAct, int kN>
+__device__ __forceinline__ void slope_run(const float (&z)[kN], float (&v)[kN]) {
 #pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_RELU);
-  } else if (act == STRADS_ACT_SIGMOID) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_SIGMOID);
-  } else if (act == STRADS_ACT_GELU) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_GELU);
-  } else if (act == STRADS_ACT_GELU_TANH) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_GELU_TANH);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) v[j] = activate(v[j], STRADS_ACT_SILU);
+  for (int j = 0; j < kN; ++j) v[j] *= slope_as<kExact, kAct>(z[j]);
+}
+template <bool kExact, int kN>
+__device__ __forceinline__ void times_slope(const float (&z)[kN], float (&v)[kN], int act) {      // v *= act'(z)
+  switch (act) {
+    case STRADS_ACT_RELU: slope_run<kExact, STRADS_ACT_RELU>(z, v); break;
+    case STRADS_ACT_SIGMOID: slope_run<kExact, STRADS_ACT_SIGMOID>(z, v); break;
+    case STRADS_ACT_GELU: slope_run<kExact, STRADS_ACT_GELU>(z, v); break;
+    case STRADS_ACT_GELU_TANH: slope_run<kExact, STRADS_ACT_GELU_TANH>(z, v); break;
+    case STRADS_ACT_SILU: slope_run<kExact, STRADS_ACT_SILU>(z, v); break;
+    default: break;
   }
 }
 
@@ -85,15 +129,17 @@ __device__ __forceinline__ void finish(const Finish& f, float z, long long a, lo
   } else {
     if (f.bias) z += load_f32(static_cast<const T*>(f.bias) + a * f.bias_a + b * f.bias_b);
     if (f.preact.p) store_f32(static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + b * f.preact.sb, z);
-    z = f.scale * activate(z, f.act);
+    float v[1] = {z};
+    activate_all<sizeof(T) == 4>(v, f.act);
+    z = f.scale * v[0];
     if (f.residual.p) z += load_f32(static_cast<const T*>(f.residual.p) + a * f.residual.sa + b * f.residual.sb);
   }
   store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + b * f.out.sb, z);
 }
 
 // ---- products with few rows on one side (linear_thin.cu) ----
-// D = A B^T with nb <= kThinMost rows in B, or in A (then swapped): every element of the long side is read once, from where it is.
-constexpr int kThinMost = 8;
+// D = A B^T with at most kThinMost rows in B, or in A (then swapped): every element of the long side is read once, from where it is.
+constexpr int kThinMost = 4;
 cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s);
 
 }  // namespace strads

@@ -21,6 +21,7 @@
 #include <mutex>
 
 #include "linear_tc.cuh"
+#include "linear_ptx.cuh"
 
 namespace strads {
 namespace {
@@ -32,7 +33,7 @@ constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
 constexpr int kThreads = 32 * (kEpiWarps + 2);
 constexpr int kSegment = 4;                // blocks of k between two emptyings of the accumulator (binary32)
 constexpr int kProducts = 6;
-constexpr uint32_t kWaitLimit = 1u << 24, kStallLimit = 1u << 14;
+constexpr uint32_t kWaitLimit = kMmaWaitLimit, kStallLimit = kMmaStallLimit;
 constexpr size_t kSmemMost = 227 * 1024;
 
 template <int kBN, int kCG>
@@ -41,82 +42,17 @@ struct Shape {
   static constexpr int kABytes = kRows * 128;
   static constexpr int kBBytes = (kCols < 64 ? 64 : kCols) * 128;          // (a box along the rows is at least 64 wide)
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = (int)((kSmemMost - 2048) / kStageBytes) < 8 ? (int)((kSmemMost - 2048) / kStageBytes) : 8;
-  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
+  static constexpr int kChunk = kBN < 128 ? 16 : 32;              // columns of a 16-bit result that a warp finishes at a time (binary32: 16)
+  static constexpr int kSlotBytes = 2048;                                 // a chunk: 32 rows of them
+  // narrow tiles read far more than they write: no shared memory for results, and two CTAs to an SM, so that up to 2 x 148 tiles
+  // are under way at once and share the memory's bandwidth evenly however they divide by 148
+  static constexpr bool kNarrow = kBN < 128;
+  static constexpr int kEpiBytes = kNarrow ? 0 : kEpiWarps * 4 * kSlotBytes;      // per warp two slots for what comes in and two for what goes out
+  static constexpr int kStages = (int)(((kNarrow ? kSmemMost / 2 - 512 : kSmemMost) - 2048 - kEpiBytes) / kStageBytes);
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpiBytes + 1024;
   static constexpr uint32_t kTmemCols = 2 * kBN < 32 ? 32 : 2 * kBN;      // two accumulators
   static_assert(kBN * kRows * 4 <= kStages * kStageBytes, "the parked sums take the ring's place");
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {         // bar: a cluster address
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
-  for (uint32_t it = 0; it < limit; ++it) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    if (ok) return true;
-  }
-  return false;
-}
-template <int kCG>
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  if (kCG == 2)
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-  else
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
-// Shared-memory descriptor, 128-byte swizzle.  k along memory: rows of 128 bytes, groups of 8 rows 1,024 bytes apart.  Rows along
-// memory: runs of 64 rows, a k per 128 bytes, groups of 8 k 1,024 bytes apart, the next 64 rows 8,192 bytes on.
-__device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, bool rows_inner) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(rows_inner ? 8192 >> 4 : 1) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-template <int kCG>
-__device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  if (kCG == 2)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-  else
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-template <int kCG>
-__device__ __forceinline__ void umma_commit(uint32_t bar) {                  // kCG = 2: on the barrier of both CTAs
-  if (kCG == 2)
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
-  else
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_load16(uint32_t taddr, uint32_t* v) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-      : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
 
 // Where a work item lies: its tile, and its share of the tile's blocks of k.
 struct Item { int ta, tb, k0, k1; };
@@ -135,43 +71,123 @@ __device__ __forceinline__ Step step_of(int k0, int len, int it) {
   return {k0 + it % len, (0x201100 >> (4 * (5 - q))) & 3, (0x021010 >> (4 * (5 - q))) & 3};
 }
 
-// Sixteen columns of one row.
-template <typename T>
-__device__ __forceinline__ void finish16(const Finish& f, const float* z, long long a, long long b0, int nb) {
-  if (f.plain) {
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+template <int kN>
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kN) : "memory"); }
+__device__ __forceinline__ void st_shared(uint32_t p, __nv_bfloat16 v) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(p), "h"(__bfloat16_as_ushort(v)) : "memory"); }
+__device__ __forceinline__ void st_shared(uint32_t p, __half v) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(p), "h"(__half_as_ushort(v)) : "memory"); }
+__device__ __forceinline__ float ld_shared(uint32_t p, float) { float v; asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p) : "memory"); return v; }
+__device__ __forceinline__ float ld_shared(uint32_t p, __nv_bfloat16) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p) : "memory");
+  return __bfloat162float(__ushort_as_bfloat16(v));
+}
+__device__ __forceinline__ float ld_shared(uint32_t p, __half) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p) : "memory");
+  return __half2float(__ushort_as_half(v));
+}
+template <typename T> __device__ __forceinline__ T as_type(float v) { T t; store_f32(&t, v); return t; }
+
+// What a warp keeps of its way through the results: the slots' use goes on from tile to tile.
+struct Epilogue {
+  uint32_t in, out, bar;                 // shared memory: two slots each; the two barriers of what comes in
+  uint32_t asked, got, put;              // chunks of the residual asked for and used; slots stored from
+};
+
+// A chunk of kC columns (b0 ..) of 32 rows (a0 ..; this lane: a0 + lane).  Through shared memory a column is one run of 32 rows,
+// which a lane writes and reads without bank conflicts; the copies to and from global memory are TMA's.  (Straight from registers, a
+// warp moves 64 bytes an instruction and the memory pipe, which the tensor cores' operands use too, takes about 20 cycles for each:
+// 8,192^3 with bias, residual and GELU 1.70 ms.)
+template <typename T, int kC>
+__device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const CUtensorMap* map_out, const CUtensorMap* map_pre, float (&v)[kC],
+                                             float bias, int a0, int b0, int lane, uint32_t limit) {
+  const Finish& f = g.f;
+  constexpr int kRow = 32 * (int)sizeof(T);
+  const long long a = a0 + lane;
+  const bool here = a < g.na;
+  const uint32_t mine = (uint32_t)lane * sizeof(T);
+  float r[kC];
+  if (!f.plain) {
+    if (g.residual_tma) {
+      const uint32_t s = e.got & 1u;
+      if (!__all_sync(0xffffffffu, mbar_wait(e.bar + 8 * s, (e.got >> 1) & 1u, limit))) return false;
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (b0 + j < nb) store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + (b0 + j) * f.out.sb, f.scale * z[j]);
-    return;
+      for (int j = 0; j < kC; ++j) r[j] = ld_shared(e.in + s * 2048 + j * kRow + mine, T());
+      ++e.got;
+      __syncwarp();
+    } else if (f.residual.p) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j)
+        r[j] = here && b0 + j < g.nb ? load_f32(static_cast<const T*>(f.residual.p) + a * f.residual.sa + (b0 + j) * f.residual.sb) : 0.f;
+    }
+    if (f.bias_b == 0) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j) v[j] += bias;
+    } else if (f.bias) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j)
+        if (b0 + j < g.nb) v[j] += load_f32(static_cast<const T*>(f.bias) + (b0 + j));
+    }
+    if (g.preact_tma) {
+      const uint32_t slot = e.out + (e.put++ & 1u) * 2048;
+      if (lane == 0) tma_stores_read<1>();
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) tma_store_2d(map_pre, slot, a0, b0);
+    } else if (f.preact.p && here) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j)
+        if (b0 + j < g.nb) store_f32(static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + (b0 + j) * f.preact.sb, v[j]);
+    }
+    activate_all<sizeof(T) == 4>(v, f.act);
+    if (f.residual.p) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j) v[j] = fmaf(f.scale, v[j], r[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kC; ++j) v[j] *= f.scale;
+    }
+  } else if (f.scale != 1.f) {
+#pragma unroll
+    for (int j = 0; j < kC; ++j) v[j] *= f.scale;
   }
-  float r[16];
+  if (g.out_tma) {
+    const uint32_t slot = e.out + (e.put++ & 1u) * 2048;
+    if (lane == 0) tma_stores_read<1>();
+    __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 16; ++j)                           // (all before the stores: out may be the residual)
-    r[j] = f.residual.p && b0 + j < nb ? load_f32(static_cast<const T*>(f.residual.p) + a * f.residual.sa + (b0 + j) * f.residual.sb) : 0.f;
-  float v[16];
+    for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) tma_store_2d(map_out, slot, a0, b0);
+  } else if (here) {
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    v[j] = z[j];
-    if (f.bias && b0 + j < nb) v[j] += load_f32(static_cast<const T*>(f.bias) + a * f.bias_a + (b0 + j) * f.bias_b);
+    for (int j = 0; j < kC; ++j)
+      if (b0 + j < g.nb) store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + (b0 + j) * f.out.sb, v[j]);
   }
-  if (f.preact.p)
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (b0 + j < nb) store_f32(static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + (b0 + j) * f.preact.sb, v[j]);
-  activate_all<16>(v, f.act);
-#pragma unroll
-  for (int j = 0; j < 16; ++j)
-    if (b0 + j < nb) store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + (b0 + j) * f.out.sb, f.scale * v[j] + r[j]);
+  return true;
 }
 
 template <typename T, int kBN, int kCG>
-__global__ void __launch_bounds__(kThreads, 1)
-k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ TcArgs g) {
+__global__ void __launch_bounds__(kThreads, kBN < 128 ? 2 : 1)
+k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+            const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ TcArgs g) {
   using S = Shape<kBN, kCG>;
   constexpr bool kPlanes = sizeof(T) == 4;
   constexpr int kHalf = kBN / 2;                         // columns of a tile that an epilogue warp reads back
   extern __shared__ unsigned char dyn[];
-  __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_tfull[2], s_tempty[2];
+  __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_tfull[2], s_tempty[2], s_in[kEpiWarps][2];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -186,6 +202,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     s_abort = 0;
     for (int i = 0; i < S::kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(tfull + 8 * i, 1); mbar_init(tempty + 8 * i, kEpiWarps * kCG); }
+    for (int i = 0; i < 2 * kEpiWarps; ++i) mbar_init(smem_u32(s_in) + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
@@ -302,14 +319,34 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   } else {
     const int quarter = warp & 3, half = warp >> 2;      // tensor memory lanes 32 quarter .. , columns half * kHalf ..
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    constexpr int kC = kPlanes ? 16 : S::kChunk, kChunks = kHalf / kC;
     uint32_t u = 0;
     bool ok = true;
+    Epilogue e;
+    e.in = tiles + S::kStages * S::kStageBytes + warp * 4 * S::kSlotBytes;
+    e.out = e.in + 2 * S::kSlotBytes;
+    e.bar = smem_u32(s_in) + 16 * warp;
+    e.asked = e.got = e.put = 0;
     for (int i = first; i < n_items && ok; i += stride) {
       const Item w = item_of(g, i, split);
-      const long long a = (long long)w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32 + lane;
-      const long long b0 = (long long)w.tb * kBN + half * kHalf;
+      const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + half * kHalf;
       const int seg = kPlanes ? kSegment : w.k1 - w.k0;
-      float acc[kPlanes ? kHalf : 16];
+      // chunks that lie in D at all
+      const int chunks = a0 < g.na && b0 < g.nb ? min(kChunks, (g.nb - b0 + kC - 1) / kC) : 0;
+      // the residual's next chunk is asked for a chunk ahead, a tile's first while its sums are still being formed
+      auto ask = [&](int c) {
+        if (g.splits == 1 && g.residual_tma && c < chunks) {
+          if (lane == 0) {
+            mbar_expect(e.bar + 8 * (e.asked & 1u), 32 * kC * (uint32_t)sizeof(T));
+            tma_load_2d(e.in + (e.asked & 1u) * 2048, &map_res, a0, b0 + c * kC, e.bar + 8 * (e.asked & 1u));
+          }
+          ++e.asked;
+        }
+      };
+      ask(0);
+      float bias = 0.f;
+      if (g.f.bias && g.f.bias_b == 0 && a0 + lane < g.na) bias = load_f32(static_cast<const T*>(g.f.bias) + (a0 + lane));
+      float acc[kPlanes ? kHalf : kC];
       if (kPlanes)
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) acc[j] = 0.f;
@@ -319,24 +356,36 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + (u & 1u) * kBN + lanes + half * kHalf;
+        if (kPlanes) {
 #pragma unroll
-        for (int c = 0; c < kHalf / 16; ++c) {
-          uint32_t v[16];
-          __syncwarp();
-          tmem_load16(d + c * 16, v);
-          tmem_wait();
-          if (kPlanes) {
+          for (int c = 0; c < kHalf / 16; ++c) {
+            uint32_t v[16];
+            tmem_load16(d + c * 16, v);
+            tmem_wait();
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[c * 16 + j] += __uint_as_float(v[j]);
-          } else if (g.splits == 1) {
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < kChunks; ++c) {
+            if (g.splits == 1 && c >= chunks) break;
+            uint32_t v[kC];
+            __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[j] = __uint_as_float(v[j]);
-            if (a < g.na) finish16<T>(g.f, acc, a, b0 + c * 16, g.nb);
-          } else {
+            for (int q = 0; q < kC / 16; ++q) tmem_load16(d + c * kC + q * 16, v + q * 16);
+            tmem_wait();
+            float x[kC];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)                 // (the ring is drained: all of it has been read by the MMAs)
-              asm volatile("st.shared.f32 [%0], %1;" ::"r"(tiles + (uint32_t)(((half * kHalf + c * 16 + j) * kRows + quarter * 32 + lane) * 4)),
-                           "f"(__uint_as_float(v[j])) : "memory");
+            for (int j = 0; j < kC; ++j) x[j] = __uint_as_float(v[j]);
+            if (g.splits == 1) {
+              ask(c + 1);
+              ok = finish_chunk<T, kC>(g, e, &map_out, &map_pre, x, bias, a0, b0 + c * kC, lane, limit);
+              if (!ok) break;
+            } else {
+#pragma unroll
+              for (int j = 0; j < kC; ++j)               // (the ring is drained: all of it has been read by the MMAs)
+                st_shared(tiles + (uint32_t)(((half * kHalf + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
+            }
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -345,17 +394,27 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       }
       if (kPlanes && ok) {
 #pragma unroll
-        for (int c = 0; c < kHalf / 16; ++c) {
+        for (int c = 0; c < kChunks; ++c) {
+          float x[kC];
+#pragma unroll
+          for (int j = 0; j < kC; ++j) x[j] = acc[c * kC + j];
           if (g.splits == 1) {
-            if (a < g.na) finish16<T>(g.f, acc + c * 16, a, b0 + c * 16, g.nb);
+            if (c < chunks && ok) {
+              ask(c + 1);
+              ok = finish_chunk<T, kC>(g, e, &map_out, &map_pre, x, bias, a0, b0 + c * kC, lane, limit);
+            }
           } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              asm volatile("st.shared.f32 [%0], %1;" ::"r"(tiles + (uint32_t)(((half * kHalf + c * 16 + j) * kRows + quarter * 32 + lane) * 4)),
-                           "f"(acc[c * 16 + j]) : "memory");
+            for (int j = 0; j < kC; ++j)
+              st_shared(tiles + (uint32_t)(((half * kHalf + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
           }
         }
       }
+    }
+    if (lane == 0) {                                     // nothing of this warp's is under way when the shared memory goes
+      for (; e.got != e.asked; ++e.got)
+        if (!mbar_wait(e.bar + 8 * (e.got & 1u), (e.got >> 1) & 1u, limit)) break;
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     __syncwarp();
@@ -392,14 +451,10 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   }
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // What is asked of the driver once per process and device.
-struct Device { bool known; int sms; int pairs; int most[9]; };      // most[n]: clusters of n CTAs that fit at once
+struct Device { bool known; int sms; int pairs; int most[9], most_narrow[9]; };      // most[n]: clusters of n CTAs that fit at once
 constexpr int kMaxDevices = 64;
 std::mutex g_mutex;
-EncodeFn g_encode;
 Device g_device[kMaxDevices];
 
 template <typename K>
@@ -436,42 +491,45 @@ cudaError_t device_of(const Device** out) {
   std::lock_guard<std::mutex> lock(g_mutex);
   Device& d = g_device[dev];
   if (!d.known) {
-    if (g_encode == nullptr) {
-      void* fn = nullptr;
-      cudaDriverEntryPointQueryResult qres;
-      if ((e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres)) != cudaSuccess) return e;
-      if (fn == nullptr || qres != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
-      g_encode = reinterpret_cast<EncodeFn>(fn);
-    }
+    if (tensor_map_encoder() == nullptr) return cudaErrorNotSupported;
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = allow_all<float>()) != cudaSuccess || (e = allow_all<__nv_bfloat16>()) != cudaSuccess || (e = allow_all<__half>()) != cudaSuccess) return e;
     d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<256, 2>::kSmem);
     if (d.pairs < 1) return cudaErrorNotSupported;
-    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<128, 1>::kSmem);
+    for (int n = 2; n <= 8; ++n) {
+      d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<128, 1>::kSmem);
+      d.most_narrow[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 64, 1>, n, Shape<64, 1>::kSmem);
+    }
     d.known = true;
   }
   *out = &d;
   return cudaSuccess;
 }
 
-// box: {64, rows} where k runs through memory, {64, 64} where the rows do.
-bool encode(CUtensorMap* map, const Planes& m, bool bf16, int box_rows) {
-  const cuuint64_t dims[3] = {(cuuint64_t)m.inner, (cuuint64_t)m.outer, (cuuint64_t)m.planes};
-  const cuuint64_t pitch = (cuuint64_t)m.ld * 2, plane = m.planes > 1 ? (cuuint64_t)m.plane * 2 : pitch;
-  const cuuint64_t strides[2] = {pitch, plane};
-  const cuuint32_t box[3] = {(cuuint32_t)kBlockK, (cuuint32_t)(m.rows_inner ? kBlockK : box_rows), 1};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return g_encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(m.p), dims, strides, box,
-                  estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+// A result, or what is laid out like it, 32 rows by `cols` columns at a time; false where TMA cannot address it.
+template <typename T>
+bool encode_result(CUtensorMap* map, const Side& m, int na, int nb, int cols) {
+  if (m.p == nullptr || (m.sa != 1 && na > 1) || ((uintptr_t)m.p & 15) != 0 || (nb > 1 && ((m.sb * (long long)sizeof(T)) % 16 != 0 || m.sb < na))) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)na, (cuuint64_t)nb};
+  const cuuint64_t strides[1] = {nb > 1 ? (cuuint64_t)m.sb * sizeof(T) : ((cuuint64_t)na * sizeof(T) + 15) / 16 * 16};
+  const cuuint32_t box[2] = {32, (cuuint32_t)cols}, estr[2] = {1, 1};
+  const CUtensorMapDataType type = sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+  return tensor_map_encoder()(map, type, 2, const_cast<void*>(m.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int kBN, int kCG>
 cudaError_t launch(const Planes& A, const Planes& B, TcArgs g, unsigned ctas, cudaStream_t s) {
   using S = Shape<kBN, kCG>;
-  alignas(64) CUtensorMap ma, mb;
-  if (!encode(&ma, A, g.bf16, kRows) || !encode(&mb, B, g.bf16, S::kCols)) return cudaErrorInvalidValue;
-  return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, g);
+  alignas(64) CUtensorMap ma, mb, mo = {}, mr = {}, mp = {};
+  if (!encode_operand(&ma, A, g.bf16, kRows) || !encode_operand(&mb, B, g.bf16, S::kCols)) return cudaErrorInvalidValue;
+  constexpr int kC = sizeof(T) == 4 ? 16 : S::kChunk;
+  if (g.splits == 1 && !S::kNarrow) {                    // (shared tiles are finished element by element)
+    g.out_tma = encode_result<T>(&mo, g.f.out, g.na, g.nb, kC);
+    g.residual_tma = encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
+    g.preact_tma = encode_result<T>(&mp, g.f.preact, g.na, g.nb, kC);
+  }
+  return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -488,17 +546,40 @@ cudaError_t launch_typed(const Device& d, const Planes& A, const Planes& B, TcAr
   const int bn = g.nb > 64 ? 128 : g.nb > 32 ? 64 : 32;
   g.tiles_a = narrow; g.tiles_b = ceil_div(g.nb, bn); g.splits = 1;
   const long long n = (long long)g.tiles_a * g.tiles_b;
-  // few tiles: as many CTAs to a tile as the GPU holds at once, each with two stages' worth of k at least
-  if (n * 2 <= d.sms)
+  // few tiles: as many CTAs to a tile as the GPU holds at once (narrow tiles: twice as many), each with four blocks of k at least
+  const int slots = bn == 128 ? d.sms : 2 * d.sms;
+  const int* most = bn == 128 ? d.most : d.most_narrow;
+  if (n * 2 <= slots)
     for (int size = 8; size >= 2; --size)
-      if (d.most[size] >= n && size * 2 <= g.blocks) { g.splits = size; break; }
-  const unsigned ctas = g.splits > 1 ? (unsigned)n * g.splits : (unsigned)(n < d.sms ? n : d.sms);
+      if (most[size] >= n && size * 4 <= g.blocks) { g.splits = size; break; }
+  const unsigned ctas = g.splits > 1 ? (unsigned)n * g.splits : (unsigned)(n < slots ? n : slots);
   if (bn == 128) return launch<T, 128, 1>(A, B, g, ctas, s);
   if (bn == 64) return launch<T, 64, 1>(A, B, g, ctas, s);
   return launch<T, 32, 1>(A, B, g, ctas, s);
 }
 
 }  // namespace
+
+EncodeFn tensor_map_encoder() {
+  static const EncodeFn found = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    return e == cudaSuccess && qres == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeFn>(fn) : nullptr;
+  }();
+  return found;
+}
+
+// box: {64, rows} where k runs through memory, {64, 64} where the rows do.
+bool encode_operand(CUtensorMap* map, const Planes& m, bool bf16, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)m.inner, (cuuint64_t)m.outer, (cuuint64_t)m.planes};
+  const cuuint64_t pitch = (cuuint64_t)m.ld * 2, plane = m.planes > 1 ? (cuuint64_t)m.plane * 2 : pitch;
+  const cuuint64_t strides[2] = {pitch, plane};
+  const cuuint32_t box[3] = {64, (cuuint32_t)(m.rows_inner ? 64 : box_rows), 1}, estr[3] = {1, 1, 1};
+  return tensor_map_encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(m.p), dims, strides,
+                              box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 cudaError_t launch_linear_tc(int type, const Planes& A, const Planes& B, long long na, long long nb, long long nk, const Finish& f,
                              unsigned int* status, bool stall, cudaStream_t s) {

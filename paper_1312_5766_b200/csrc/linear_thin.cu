@@ -3,10 +3,12 @@
 // cores: a tile of theirs would be nearly empty, and binary32 would have to be split first.
 //
 //   k along memory (k_thin_k): a warp takes rows, a lane every 32nd group of 16 bytes of them; lanes are added by shuffles.
-//   rows along memory (k_thin_rows): a lane takes the rows of 16 bytes, a warp every eighth k; warps are added through shared memory.
+//   rows along memory (k_thin_rows): a lane takes the rows of 16 bytes (or of 4, where there are few), a warp every 16th k; warps
+//   are added through shared memory.
 //
-// The short side is staged in shared memory as binary32.  Where the rows alone do not fill the GPU, the CTAs of a cluster share k
-// and add through distributed shared memory, in the order of the CTAs.
+// What hides the memory's latency is the number of loads under way: eight per lane, and enough warps; where the rows alone do not
+// make enough of them, the warps of a CTA and the CTAs of a cluster share k and add through (distributed) shared memory, in a fixed order.
+// The short side is staged in shared memory as binary32, or (k along memory, up to four rows) read through L1 as it is.
 #include <mutex>
 
 #include "linear.cuh"
@@ -14,13 +16,13 @@
 namespace strads {
 namespace {
 
-constexpr int kThreads = 256, kWarps = 8;
+constexpr int kThreads = 256, kWarps = 8;      // k_thin_k
 constexpr int kStageFloats = 8192;             // of the short side in shared memory at a time
 
 struct Thin {
   Operand L, S;                                // the long and the short side
   long long nl, nk;
-  int ns, splits, swapped, vec;                // swapped: the long side is D's b
+  int ns, splits, swapped, vec, svec;          // swapped: the long side is D's b; vec, svec: 16-byte accesses to the long, the short side
   int wk;                                      // k_thin_k: warps of a CTA that share a row's k (1 or 8)
   Finish f;
 };
@@ -41,17 +43,34 @@ __device__ __forceinline__ void finish_thin(const Thin& t, float v, long long l,
   if (t.swapped) finish<T>(t.f, v, s, l); else finish<T>(t.f, v, l, s);
 }
 
-// 16 bytes of T as floats.
-template <typename T> struct Vec { static constexpr int kN = 16 / sizeof(T); T x[kN]; };
-template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, float (&v)[16 / sizeof(T)]) {
-  const uint4 raw = __ldg(reinterpret_cast<const uint4*>(p));
-  const T* x = reinterpret_cast<const T*>(&raw);
+// kBytes of T, as they are and as floats.
+template <int kBytes> struct Raw;
+template <> struct Raw<16> { uint4 v; };
+template <> struct Raw<4> { unsigned int v; };
+template <int kBytes>
+__device__ __forceinline__ Raw<kBytes> load_raw(const void* p) {
+  Raw<kBytes> r;
+  r.v = __ldg(static_cast<const decltype(r.v)*>(p));
+  return r;
+}
+// The long side's: read once, so not kept in L1.  (volatile: a batch of them is issued before the first is used, as written)
+template <int kBytes>
+__device__ __forceinline__ Raw<kBytes> load_once(const void* p) {
+  Raw<kBytes> r;
+  if constexpr (kBytes == 16)
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.v.x), "=r"(r.v.y), "=r"(r.v.z), "=r"(r.v.w) : "l"(p));
+  else
+    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r.v) : "l"(p));
+  return r;
+}
+template <typename T, int kBytes>
+__device__ __forceinline__ void to_floats(const Raw<kBytes>& r, float (&v)[kBytes / sizeof(T)]) {
+  const T* x = reinterpret_cast<const T*>(&r);
 #pragma unroll
-  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) v[i] = load_f32(x + i);
+  for (int i = 0; i < (int)(kBytes / sizeof(T)); ++i) v[i] = load_f32(x + i);
 }
 
-// The share of k of this CTA, and its rows.
+// The share of k of this CTA.
 __device__ __forceinline__ void share(const Thin& t, long long unit, long long* k0, long long* k1) {
   const long long units = (t.nk + unit - 1) / unit, r = t.splits > 1 ? blockIdx.x % t.splits : 0;
   *k0 = units * r / t.splits * unit;
@@ -61,17 +80,18 @@ __device__ __forceinline__ void share(const Thin& t, long long unit, long long* 
 // S[s][k0 .. k0 + n) -> shared memory, [k][kT] or [kT][n], noughts behind the last row.
 template <typename T, int kT, bool kByK>
 __device__ __forceinline__ void stage_short(const Thin& t, long long k0, int n, float* sh, int pitch) {
-  for (int i = threadIdx.x; i < n * kT; i += kThreads) {
+  for (int i = threadIdx.x; i < n * kT; i += blockDim.x) {
     const int s = t.S.ks == 1 ? i / n : i % kT, k = t.S.ks == 1 ? i % n : i / kT;
     const float v = s < t.ns ? load_f32(static_cast<const T*>(t.S.p) + s * t.S.rs + (k0 + k) * t.S.ks) : 0.f;
     sh[kByK ? k * kT + s : s * pitch + k] = v;
   }
 }
 
-template <typename T, int kT, int kR>
+// kDirect: the short side is read as it is (16-byte accesses to both sides).
+template <typename T, int kT, int kR, bool kDirect>
 __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thin t) {
-  constexpr int kV = 16 / sizeof(T), kStage = kStageFloats / kT;
-  __shared__ __align__(16) float sh[kStageFloats];
+  constexpr int kV = 16 / sizeof(T), kStage = kStageFloats / kT, kU = kR * kT <= 2 ? 8 : 4;
+  __shared__ __align__(16) float sh[kDirect ? 4 : kStageFloats];
   __shared__ float red[kWarps][kR * kT];
   __shared__ float sum[kWarps][kR * kT];
   chain_begin();
@@ -79,42 +99,64 @@ __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thi
   const long long group = (long long)(blockIdx.x / t.splits);
   const long long l0 = t.wk == 1 ? (group * kWarps + warp) * kR : group * kR;
   long long k0, k1;
-  share(t, kStage < 1024 ? kStage : 1024, &k0, &k1);
+  share(t, 256, &k0, &k1);
   float acc[kR][kT] = {};
   const T* row[kR];
 #pragma unroll
   for (int r = 0; r < kR; ++r) row[r] = static_cast<const T*>(t.L.p) + min(l0 + r, t.nl - 1) * t.L.rs;
-  for (long long kb = k0; kb < k1; kb += kStage) {
-    const int n = (int)min((long long)kStage, k1 - kb);
-    __syncthreads();
-    stage_short<T, kT, false>(t, kb, n, sh, kStage);
-    __syncthreads();
-    const int at = t.wk == 1 ? lane : warp * 32 + lane, step = t.wk == 1 ? 32 : 256;
-    if (t.vec) {
-      const int groups = n / kV;
-#pragma unroll 4
-      for (int i = at; i < groups; i += step) {
-        float x[kR][kV];
+  const int at = t.wk == 1 ? lane : warp * 32 + lane, step = t.wk == 1 ? 32 : 256;
+  const int stage = kDirect ? 0x40000000 : kStage;
+  for (long long kb = k0; kb < k1; kb += stage) {
+    const int n = (int)min((long long)stage, k1 - kb);
+    if (!kDirect) {
+      __syncthreads();
+      stage_short<T, kT, false>(t, kb, n, sh, kStage);
+      __syncthreads();
+    }
+    const int groups = t.vec ? n / kV : 0;
+    for (int i0 = at; i0 < groups; i0 += step * kU) {
+      Raw<16> x[kU][kR], y[kU][kDirect ? kT : 1];
 #pragma unroll
-        for (int r = 0; r < kR; ++r) load_vec(row[r] + kb + (long long)i * kV, x[r]);
+      for (int u = 0; u < kU; ++u) {
+        const long long i = min(i0 + u * step, groups - 1);      // (one past the end reads the last again, for nothing)
+#pragma unroll
+        for (int r = 0; r < kR; ++r) x[u][r] = load_once<16>(row[r] + kb + i * kV);
+        if (kDirect)
+#pragma unroll
+          for (int s = 0; s < kT; ++s) y[u][s] = load_raw<16>(static_cast<const T*>(t.S.p) + min(s, t.ns - 1) * t.S.rs + kb + i * kV);
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = i0 + u * step;
+        if (i >= groups) break;
+        float xf[kR][kV];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) to_floats<T, 16>(x[u][r], xf[r]);
 #pragma unroll
         for (int s = 0; s < kT; ++s) {
-          float y[kV];
+          float yf[kV];
+          if (kDirect) {
+            to_floats<T, 16>(y[u][kDirect ? s : 0], yf);
+          } else {
 #pragma unroll
-          for (int v = 0; v < kV; v += 4) *reinterpret_cast<float4*>(y + v) = *reinterpret_cast<const float4*>(sh + s * kStage + i * kV + v);
+            for (int v = 0; v < kV; v += 4) *reinterpret_cast<float4*>(yf + v) = *reinterpret_cast<const float4*>(sh + s * kStage + i * kV + v);
+          }
 #pragma unroll
           for (int r = 0; r < kR; ++r)
 #pragma unroll
-            for (int v = 0; v < kV; ++v) acc[r][s] = fmaf(x[r][v], y[v], acc[r][s]);
+            for (int v = 0; v < kV; ++v) acc[r][s] = fmaf(xf[r][v], yf[v], acc[r][s]);
         }
       }
     }
-    for (int k = (t.vec ? n / kV * kV : 0) + at; k < n; k += step) {
+    for (int k = groups * kV + at; k < n; k += step) {
 #pragma unroll
       for (int r = 0; r < kR; ++r) {
         const float x = load_f32(row[r] + (kb + k) * t.L.ks);
 #pragma unroll
-        for (int s = 0; s < kT; ++s) acc[r][s] = fmaf(x, sh[s * kStage + k], acc[r][s]);
+        for (int s = 0; s < kT; ++s) {
+          const float y = !kDirect ? sh[s * kStage + k] : load_f32(static_cast<const T*>(t.S.p) + min(s, t.ns - 1) * t.S.rs + kb + k);
+          acc[r][s] = fmaf(x, y, acc[r][s]);
+        }
       }
     }
   }
@@ -126,6 +168,12 @@ __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thi
       for (int o = 16; o > 0; o >>= 1) acc[r][s] += __shfl_xor_sync(0xffffffffu, acc[r][s], o);
       if (lane == 0) red[warp][r * kT + s] = acc[r][s];
     }
+  if (t.wk == 1 && t.splits == 1) {                      // a warp finishes its own rows
+    __syncwarp();
+    for (int e = lane; e < kR * kT; e += 32)
+      if (l0 + e / kT < t.nl && e % kT < t.ns) finish_thin<T>(t, red[warp][e], l0 + e / kT, e % kT);
+    return;
+  }
   // sums of the CTA: one set per warp, or one for all of them
   __syncthreads();
   const int sets = t.wk == 1 ? kWarps : 1;
@@ -149,9 +197,10 @@ __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thi
   if (t.splits > 1) cluster_sync();                      // nobody leaves while its sums may be read
 }
 
-template <typename T, int kT>
-__global__ void __launch_bounds__(kThreads) k_thin_rows(const __grid_constant__ Thin t) {
-  constexpr int kV = 16 / sizeof(T), kTile = 32 * kV, kStage = kStageFloats / kT;
+constexpr int kRowWarps = 16, kRowThreads = 32 * kRowWarps;
+template <typename T, int kT, int kBytes>
+__global__ void __launch_bounds__(kRowThreads) k_thin_rows(const __grid_constant__ Thin t) {
+  constexpr int kV = kBytes / sizeof(T), kTile = 32 * kV, kStage = kStageFloats / kT, kU = 8;
   __shared__ __align__(16) float sh[kStageFloats];
   float* sum = sh;                                       // [kT][kTile], when the last of the short side has been used
   static_assert(kT * kTile <= kStageFloats, "the sums take the stage's place");
@@ -159,34 +208,46 @@ __global__ void __launch_bounds__(kThreads) k_thin_rows(const __grid_constant__ 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long l0 = (long long)(blockIdx.x / t.splits) * kTile, l = l0 + lane * kV;
   long long k0, k1;
-  share(t, 64, &k0, &k1);
+  share(t, 16, &k0, &k1);
   const bool whole = t.vec && l + kV <= t.nl;
   float acc[kT][kV] = {};
+  auto add = [&](int k, const float (&x)[kV]) {
+#pragma unroll
+    for (int s = 0; s < kT; ++s) {
+      const float y = sh[k * kT + s];
+#pragma unroll
+      for (int v = 0; v < kV; ++v) acc[s][v] = fmaf(x[v], y, acc[s][v]);
+    }
+  };
   for (long long kb = k0; kb < k1; kb += kStage) {
     const int n = (int)min((long long)kStage, k1 - kb);
     __syncthreads();
     stage_short<T, kT, true>(t, kb, n, sh, 0);
     __syncthreads();
     const T* at = static_cast<const T*>(t.L.p) + kb * t.L.ks + l * t.L.rs;
-#pragma unroll 4
-    for (int k = warp; k < n; k += kWarps) {
-      float x[kV];
-      if (whole) {
-        load_vec(at + k * t.L.ks, x);
-      } else {
+    if (whole) {
+      for (int i0 = warp; i0 < n; i0 += kRowWarps * kU) {
+        Raw<kBytes> x[kU];
 #pragma unroll
-        for (int v = 0; v < kV; ++v) x[v] = l + v < t.nl ? load_f32(at + k * t.L.ks + v * t.L.rs) : 0.f;
+        for (int u = 0; u < kU; ++u) x[u] = load_once<kBytes>(at + min(i0 + u * kRowWarps, n - 1) * t.L.ks);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          if (i0 + u * kRowWarps >= n) break;
+          float xf[kV];
+          to_floats<T, kBytes>(x[u], xf);
+          add(i0 + u * kRowWarps, xf);
+        }
       }
-      float y[kT];
+    } else if (l < t.nl) {
+      for (int k = warp; k < n; k += kRowWarps) {
+        float xf[kV];
 #pragma unroll
-      for (int s = 0; s < kT; ++s) y[s] = sh[k * kT + s];
-#pragma unroll
-      for (int s = 0; s < kT; ++s)
-#pragma unroll
-        for (int v = 0; v < kV; ++v) acc[s][v] = fmaf(x[v], y[s], acc[s][v]);
+        for (int v = 0; v < kV; ++v) xf[v] = l + v < t.nl ? load_f32(at + k * t.L.ks + v * t.L.rs) : 0.f;
+        add(k, xf);
+      }
     }
   }
-  for (int w = 0; w < kWarps; ++w) {                     // in the order of the warps
+  for (int w = 0; w < kRowWarps; ++w) {                  // in the order of the warps
     __syncthreads();
     if (warp == w)
 #pragma unroll
@@ -199,7 +260,7 @@ __global__ void __launch_bounds__(kThreads) k_thin_rows(const __grid_constant__ 
   }
   if (t.splits > 1) cluster_sync(); else __syncthreads();
   const int rank = t.splits > 1 ? (int)(blockIdx.x % t.splits) : 0;
-  for (int i = rank * kThreads + threadIdx.x; i < kT * kTile; i += kThreads * t.splits) {
+  for (int i = rank * kRowThreads + threadIdx.x; i < kT * kTile; i += kRowThreads * t.splits) {
     const int s = i / kTile, j = i % kTile;              // row j of the tile is lane j / kV's, its (j % kV)-th
     if (l0 + j >= t.nl || s >= t.ns) continue;
     const float* p = sum + s * kTile + (j % kV) * 32 + j / kV;
@@ -211,30 +272,43 @@ __global__ void __launch_bounds__(kThreads) k_thin_rows(const __grid_constant__ 
   if (t.splits > 1) cluster_sync();
 }
 
-bool vec_ok(const void* p, long long pitch, size_t size) { return ((uintptr_t)p & 15) == 0 && (pitch * size) % 16 == 0; }
+bool vec_ok(const void* p, long long pitch, long long rows, size_t size) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || (pitch * (long long)size) % 16 == 0); }
 
+template <typename T, int kT, int kBytes>
+cudaError_t launch_rows(const Thin& t, long long tiles, cudaStream_t s) {
+  if (t.splits > 8) {                                    // (clusters of more than 8 CTAs: the device takes them on request)
+    const cudaError_t e = cudaFuncSetAttribute(k_thin_rows<T, kT, kBytes>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_chained_cluster(k_thin_rows<T, kT, kBytes>, dim3((unsigned)(tiles * t.splits)), kRowThreads, 0, s, t.splits, t);
+}
 template <typename T, int kT>
 cudaError_t launch(Thin t, int sms, cudaStream_t s) {
   const bool along_k = t.L.ks == 1 || t.L.rs != 1;
+  t.splits = 1;
   if (along_k) {
-    t.vec = t.L.ks == 1 && (t.nl == 1 || vec_ok(t.L.p, t.L.rs, sizeof(T))) && ((uintptr_t)t.L.p & 15) == 0;
+    t.vec = t.L.ks == 1 && vec_ok(t.L.p, t.L.rs, t.nl, sizeof(T));
+    t.svec = t.S.ks == 1 && vec_ok(t.S.p, t.S.rs, t.ns, sizeof(T));
     constexpr int kR = kT >= 4 ? 2 : 1;
     const long long warps = (t.nl + kR - 1) / kR;
-    t.wk = warps >= 4 * sms ? 1 : kWarps;                // few rows: the warps of a CTA share them
+    t.wk = warps >= 8ll * sms ? 1 : kWarps;              // few rows: the warps of a CTA share them
     const long long groups = t.wk == 1 ? (warps + kWarps - 1) / kWarps : warps;
-    t.splits = 1;
     while (t.splits < 8 && groups * t.splits * 2 <= 2 * sms && t.nk >= 4096ll * t.splits) t.splits *= 2;
-    return launch_chained_cluster(k_thin_k<T, kT, kR>, dim3((unsigned)(groups * t.splits)), kThreads, 0, s, t.splits, t);
+    const dim3 grid((unsigned)(groups * t.splits));
+    if (t.vec && t.svec) return launch_chained_cluster(k_thin_k<T, kT, kR, true>, grid, kThreads, 0, s, t.splits, t);
+    return launch_chained_cluster(k_thin_k<T, kT, kR, false>, grid, kThreads, 0, s, t.splits, t);
   }
-  t.vec = vec_ok(t.L.p, t.L.ks, sizeof(T));
-  const long long tiles = (t.nl + 32 * (16 / sizeof(T)) - 1) / (32 * (16 / sizeof(T)));
-  t.splits = 1;
-  while (t.splits < 8 && tiles * t.splits * 2 <= 4 * sms && t.nk >= 256ll * t.splits) t.splits *= 2;
-  return launch_chained_cluster(k_thin_rows<T, kT>, dim3((unsigned)(tiles * t.splits)), kThreads, 0, s, t.splits, t);
+  t.vec = vec_ok(t.L.p, t.L.ks, t.nk, sizeof(T));
+  // 16 bytes of a row per lane where that leaves enough CTAs, 4 otherwise; then as many CTAs to a tile as keep four on every SM
+  const long long wide = (t.nl + 512 / (int)sizeof(T) - 1) / (512 / (int)sizeof(T)), narrow = (t.nl + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T));
+  const bool few = wide * 16 < 2ll * sms;
+  const long long tiles = few ? narrow : wide;
+  while (t.splits < 16 && tiles * t.splits < 4ll * sms && t.nk >= 512ll * t.splits) t.splits *= 2;
+  return few ? launch_rows<T, kT, 4>(t, tiles, s) : launch_rows<T, kT, 16>(t, tiles, s);
 }
 template <typename T>
 cudaError_t by_short(const Thin& t, int sms, cudaStream_t s) {
-  return t.ns == 1 ? launch<T, 1>(t, sms, s) : t.ns == 2 ? launch<T, 2>(t, sms, s) : t.ns <= 4 ? launch<T, 4>(t, sms, s) : launch<T, 8>(t, sms, s);
+  return t.ns == 1 ? launch<T, 1>(t, sms, s) : t.ns == 2 ? launch<T, 2>(t, sms, s) : launch<T, 4>(t, sms, s);
 }
 
 }  // namespace

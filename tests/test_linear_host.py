@@ -14,7 +14,7 @@ def b():
 
 def _config(b, **kw):
     c = b.LinearConfig(type=1, activation=3, n_rows=100, n_in=200, n_out=300, scale=1.0)
-    c.x, c.w = b.Matrix(0x100000, 200, 1), b.Matrix(0x200000, 200, 1)      # never dereferenced
+    c.x, c.x_row_stride, c.x_col_stride, c.w, c.w_row_stride, c.w_col_stride = 0x100000, 200, 1, 0x200000, 200, 1      # never dereferenced
     c.workspace, c.workspace_bytes = 0x10000000, 1 << 40
     for k, v in kw.items():
         setattr(c, k, v)
@@ -48,8 +48,8 @@ def test_bad_configurations(b, kw, which):
 @pytest.mark.parametrize("which", ["forward", "backward"])
 def test_bad_operands(b, which):
     for x in (b.Matrix(None, 200, 1), b.Matrix(0x100001, 200, 1), b.Matrix(0x100000, -200, 1), b.Matrix(0x100000, 200, -1)):
-        assert _call(b, _config(b, x=x), which) == -1
-        assert _call(b, _config(b, w=x), which) == -1
+        for side in "xw":
+            assert _call(b, _config(b, **{side: x.data, side + "_row_stride": x.row_stride, side + "_col_stride": x.col_stride}), which) == -1
     for n in ("n_rows", "n_in", "n_out"):
         assert _call(b, _config(b, **{n: 1 << 31}), which) == -7
 
@@ -81,11 +81,11 @@ def test_workspace(b):
     assert query(C.byref(c)) == 0 and need[1] > 0
     c.workspace_bytes = need[1] - 1
     assert _call(b, c, "backward") == -3
-    c.workspace = None
+    c.workspace, c.workspace_bytes = None, need[1]
     assert _call(b, c, "backward") == -1
     # no rows: nothing to do, whatever the pointers
     c = _config(b, n_rows=0)
-    c.x.data = None
+    c.x = None
     assert query(C.byref(c)) == 0
     assert lib.strads_linear_forward(C.byref(c), None, None, None, None) == 0
     assert lib.strads_linear_backward(C.byref(_config(b)), C.byref(b.Matrix(0x300000, 300, 1)), C.byref(b.Matrix(0x400000, 300, 1)), None, None, None) == 0
