@@ -155,8 +155,8 @@ bool vec_rows(const void* p, long long pitch, long long rows, size_t size) {
 }
 
 // `unknown`: where the matrix lies is not known yet (a workspace query), so that it has to be taken for one that is copied.
-Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unknown = false) {
-  const bool rows_inner = m.ks != 1 && (m.rs == 1 || rows == 1) && nk > 1;
+Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unknown = false, bool k_inner = false) {
+  const bool rows_inner = !k_inner && m.ks != 1 && (m.rs == 1 || rows == 1) && nk > 1;
   Planes p = {};
   p.rows_inner = rows_inner;
   p.inner = rows_inner ? rows : nk;
@@ -170,6 +170,7 @@ Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unkno
   }
   p.ld = (p.inner + 7) / 8 * 8;
   p.plane = p.outer * p.ld;
+  if (unknown && p.inner * ((p.outer + 7) / 8 * 8) > p.plane) p.plane = p.inner * ((p.outer + 7) / 8 * 8);      // (either order)
   void* dst = c.take((size_t)p.plane * p.planes * 2);
   p.p = dst;
   if (!c.run || c.err != cudaSuccess) return p;
@@ -210,16 +211,17 @@ void product(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
     if (c.run && c.err == cudaSuccess) c.err = launch_linear_thin(c.type, a, b, na, nb, nk, f, c.stream);
     return;
   }
-  // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 64
-  // rows, where planes in memory cost 16)
+  // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 32 or 48
+  // rows, most of them from L2, where planes in memory cost 16)
   const bool b_long = na < nb || (na == nb && B.order < A.order);
-  const Operand& l = b_long ? b : a;
-  if (c.size == 4 && (b_long ? na : nb) <= kSplitMost && (l.rs == 1 || l.ks == 1)) {
-    const long long nl = b_long ? nb : na, ns = b_long ? na : nb;
-    const Planes p = b_long ? side_of(c, A, ta) : side_of(c, B, tb);
+  const Operand &l = b_long ? b : a, &sh = b_long ? a : b;
+  const long long nl = b_long ? nb : na, ns = b_long ? na : nb;
+  const bool unknown = (b_long ? B : A).unknown;         // (a query: room for either way)
+  if (c.size == 4 && ns <= kSplitMost && (unknown || linear_split_takes(l, nl, nk))) {
+    const Planes p = bring(c, sh, ns, nk, false, true);
     void* ws = c.take(linear_split_workspace(nl, ns, nk));
     if (c.run && c.err == cudaSuccess) c.err = launch_linear_split(l, p, nl, ns, nk, b_long, f, ws, c.status, c.stall, c.stream);
-    return;
+    if (!unknown) return;
   }
   const Planes pa = side_of(c, A, ta), pb = side_of(c, B, tb);
   if (c.run && c.err == cudaSuccess) c.err = launch_linear_tc(c.type, pa, pb, na, nb, nk, f, c.status, c.stall, c.stream);

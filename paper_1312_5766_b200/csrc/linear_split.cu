@@ -1,11 +1,14 @@
 // binary32 products with few rows on one side (5 to 128): the margins of a path of fits, a gradient for some responses.  Bound by
 // reading the long side once, so it is read where it is, 4 bytes an element, and split into three bfloat16 planes on its way into
-// shared memory; the short side comes as planes in memory (a few hundred rows at most, written by the pass before).
+// tensor memory; the short side comes as planes in memory (written by the pass before).
 //
-// A tile is 128 rows of the long side by kBN = 32 or 64 of the short one.  Eight warps load a tile's block of 64 k (two blocks ahead, in
-// registers), split it and store it in the layout that the tensor cores read (128-byte swizzle; rows or k along memory, as in global
-// memory); one thread brings the short side's block by TMA; one issues the six largest of the nine products of planes, smallest first;
-// four warps empty the accumulator into registers every kSegment blocks (the tensor cores' additions truncate) and add there.
+// A tile is 128 rows of the long side by kBN = 32 or 48 of the short one.  One thread brings blocks of 64 k by TMA, the long side's as it is (the
+// ring holds 160 KB of it: what hides the memory's latency); eight warps, a lane per row, split them and put the planes into tensor
+// memory, which the tensor cores take their A operand from: shared memory, whose bandwidth would otherwise bound the kernel, is written and
+// read once for every element.  One thread issues the products.  The short side's planes lie one behind the other as rows of B, so three
+// MMAs form the six largest of the nine products of planes, sorted by size into three accumulators:
+//   L0 [S0 S1 S2] -> [c0 c1 c2],   L1 [S0 S1] -> [c1 c2],   L2 [S0] -> [c2],   D = c0 + (c1 + c2).
+// Four warps empty them into registers every kSegment blocks (the tensor cores' additions truncate) and add there.
 //
 // The blocks of all tiles, one tile after another, are dealt out evenly: every CTA takes a run of them, so that all SMs finish together
 // however the tiles divide.  A tile that falls to more than one CTA is left as partial sums in the workspace and finished by a second kernel, in the
@@ -16,18 +19,24 @@
 namespace strads {
 namespace {
 
-constexpr int kRows = 128, kBlockK = 64, kPlane = 16384, kShortPlane = 8192, kStageBytes = 3 * (kPlane + kShortPlane), kStages = 3;
-constexpr int kEpiWarps = 4, kLoadWarps = 8, kTmaWarp = 12, kMmaWarp = 13, kThreads = 32 * 14;
-constexpr int kLoadThreads = 32 * kLoadWarps, kGroups = kRows * kBlockK / 8 / kLoadThreads;      // groups of 8 neighbours per thread and block
+constexpr int kRows = 128, kBlockK = 64, kLongBytes = kRows * kBlockK * 4;
+constexpr int kEpiWarps = 4, kSplitWarps = 8, kTmaWarp = 12, kMmaWarp = 13, kThreads = 32 * 14;
 constexpr int kSegment = 4;
 constexpr int kMostCtas = 148;           // (a GPU with fewer SMs takes them in turn)
-constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
+
+template <int kBN>
+struct Sizes {
+  static constexpr int kShortBytes = 3 * kBN * 128;
+  static constexpr int kStageBytes = kLongBytes + kShortBytes;
+  static constexpr int kStages = (227 * 1024 - 2048) / kStageBytes;
+  static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
+  static constexpr uint32_t kD = 3 * kBN, kA = 2 * kD;      // tensor memory: two sets of accumulators, then two of the long side's planes (96 columns each)
+  static_assert(kA + 2 * 96 <= 512 && kShortBytes % 1024 == 0, "");
+};
 
 struct SplitArgs {
-  Operand L;
-  long long nk;
   int nl, ns, blocks, tiles_l, tiles_s, ctas;
-  int l_rows_inner, s_rows_inner, vec, long_is_b, stall;
+  int l_rows_inner, long_is_b, stall;
   float* partial;                        // [2 ctas][kBN][128]
   unsigned int* status;
   Finish f;
@@ -40,29 +49,56 @@ __device__ __forceinline__ void tile_of(const SplitArgs& g, int t, int* tl, int*
 __device__ __forceinline__ void finish_split(const SplitArgs& g, float v, long long l, long long s) {
   if (g.long_is_b) finish<float>(g.f, v, s, l); else finish<float>(g.f, v, l, s);
 }
+// Counts through the blocks of a run: tile and block of k.
+struct Walk {
+  int tile, block;
+  __device__ __forceinline__ Walk(const SplitArgs& g, long long u) : tile((int)(u / g.blocks)), block((int)(u % g.blocks)) {}
+  __device__ __forceinline__ void next(const SplitArgs& g) { if (++block == g.blocks) { block = 0; ++tile; } }
+};
 
-struct Held { float x[kGroups][8]; };    // what a loading thread holds of a block
+__device__ __forceinline__ void tma_load_raw(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// D (+)= A[tensor memory] B[shared memory]^T, K = 16: eight columns of A, two k in each.
+__device__ __forceinline__ void umma_a_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+                 "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
 template <int kBN>
-__global__ void __launch_bounds__(kThreads, 1) k_linear_split(const __grid_constant__ CUtensorMap map_s, const __grid_constant__ SplitArgs g) {
+__global__ void __launch_bounds__(kThreads, 1)
+k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ SplitArgs g) {
+  using Z = Sizes<kBN>;
+  constexpr int kStages = Z::kStages;
   extern __shared__ unsigned char dyn[];
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_tfull[2], s_tempty[2];
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_afull[2], s_aempty[2], s_tfull[2], s_tempty[2];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
-  constexpr uint32_t kTmemCols = 2 * kBN;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t tiles = (smem_u32(dyn) + 1023u) & ~1023u;
-  const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), tfull = smem_u32(s_tfull), tempty = smem_u32(s_tempty);
+  const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
+  const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), afull = smem_u32(s_afull), aempty = smem_u32(s_aempty), tfull = smem_u32(s_tfull),
+                 tempty = smem_u32(s_tempty);
   const uint32_t limit = g.stall ? kMmaStallLimit : kMmaWaitLimit;
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, kLoadWarps + 1); mbar_init(empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(tfull + 8 * i, 1); mbar_init(tempty + 8 * i, kEpiWarps); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(afull + 8 * i, kSplitWarps / 2); mbar_init(aempty + 8 * i, 1);
+      mbar_init(tfull + 8 * i, 1); mbar_init(tempty + 8 * i, kEpiWarps);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_l) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_s) : "memory");
   }
   if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -70,128 +106,119 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear_split(const __grid_const
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = s_tmem;
   chain_begin();
-  const long long u0 = start_of(g, (int)blockIdx.x), u1 = start_of(g, (int)blockIdx.x + 1);
+  const long long u0 = start_of(g, (int)blockIdx.x);
+  const int run = (int)(start_of(g, (int)blockIdx.x + 1) - u0);
+  Walk at(g, u0);
 
-  if (warp >= kEpiWarps && warp < kEpiWarps + kLoadWarps) {
-    const int t = (int)threadIdx.x - 32 * kEpiWarps;
-    bool ok = true;
-    auto load = [&](long long u, Held& h) {
-      int tl, ts;
-      tile_of(g, (int)(u / g.blocks), &tl, &ts);
-      const long long l0 = (long long)tl * kRows, k0 = u % g.blocks * kBlockK;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const int q = t + i * kLoadThreads;
-        // eight neighbours of one row (k along memory: 8 groups a row) or one k (rows along memory: 16 groups)
-        const long long l = l0 + (g.l_rows_inner ? q % 16 * 8 : q / 8), k = k0 + (g.l_rows_inner ? q / 16 : q % 8 * 8);
-        const long long left = (g.l_rows_inner ? g.nl - l : g.nk - k);
-        const float* p = static_cast<const float*>(g.L.p) + l * g.L.rs + k * g.L.ks;
-        const bool there = g.l_rows_inner ? k < g.nk : l < g.nl;
-        if (g.vec && there && left >= 8) {
-#pragma unroll
-          for (int j = 0; j < 8; j += 4)
-            asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(h.x[i][j]), "=f"(h.x[i][j + 1]), "=f"(h.x[i][j + 2]), "=f"(h.x[i][j + 3]) : "l"(p + j));
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) h.x[i][j] = there && j < left ? __ldg(p + j) : 0.f;
-        }
-      }
-    };
-    auto store = [&](long long n, const Held& h) {
-      const uint32_t s = (uint32_t)(n % kStages), at = tiles + s * kStageBytes;
-      ok = !s_abort && mbar_wait(empty + 8 * s, ((uint32_t)(n / kStages) & 1u) ^ 1u, limit);
-      ok = __all_sync(0xffffffffu, ok) && !g.stall;
-      if (!ok) return;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const int q = t + i * kLoadThreads;
-        const uint32_t place = g.l_rows_inner ? (uint32_t)((q % 16 / 8) * 8192 + (q / 16) * 128 + (((q % 8) ^ (q / 16 % 8)) << 4))
-                                              : (uint32_t)((q / 8) * 128 + (((q % 8) ^ (q / 8 % 8)) << 4));
-        uint32_t w[4][3];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) split_pair(h.x[i][2 * j], h.x[i][2 * j + 1], w[j]);
-#pragma unroll
-        for (int p = 0; p < 3; ++p)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + p * kPlane + place), "r"(w[0][p]), "r"(w[1][p]), "r"(w[2][p]), "r"(w[3][p]) : "memory");
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + 8 * s) : "memory");
-    };
-    Held a, b;
-    if (u0 < u1) load(u0, a);
-    if (u0 + 1 < u1) load(u0 + 1, b);
-    for (long long u = u0; u < u1 && ok; u += 2) {
-      store(u - u0, a);
-      if (u + 2 < u1) load(u + 2, a);
-      if (ok && u + 1 < u1) {
-        store(u + 1 - u0, b);
-        if (u + 3 < u1) load(u + 3, b);
-      }
-    }
-    if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
-    __syncwarp();
-  } else if (warp == kTmaWarp) {
+  if (warp == kTmaWarp) {
     if (lane == 0) {
       bool ok = true;
-      const uint32_t bytes = 3u * (uint32_t)((g.s_rows_inner ? 64 : kBN) * 128);
-      long long n = 0;
-      for (long long u = u0; u < u1; ++u, ++n) {
-        const uint32_t s = (uint32_t)(n % kStages);
+      int n = 0;
+      for (; n < run; ++n, at.next(g)) {
+        const uint32_t s = (uint32_t)(n % kStages), to = ring + s * Z::kStageBytes;
         ok = !s_abort && mbar_wait(empty + 8 * s, ((uint32_t)(n / kStages) & 1u) ^ 1u, limit) && !g.stall;
         if (!ok) break;
         int tl, ts;
-        tile_of(g, (int)(u / g.blocks), &tl, &ts);
-        const int k0 = (int)(u % g.blocks) * kBlockK, r0 = ts * kBN;
-        mbar_expect(full + 8 * s, bytes);
+        tile_of(g, at.tile, &tl, &ts);
+        const int k0 = at.block * kBlockK, l0 = tl * kRows;
+        mbar_expect(full + 8 * s, (uint32_t)Z::kStageBytes);
+        if (g.l_rows_inner) {
+          tma_load_raw(to, &map_l, l0, k0, full + 8 * s);
+        } else {
+          tma_load_raw(to, &map_l, k0, l0, full + 8 * s);
+          tma_load_raw(to + kLongBytes / 2, &map_l, k0 + 32, l0, full + 8 * s);
+        }
 #pragma unroll
-        for (int p = 0; p < 3; ++p)
-          tma_load<1>(tiles + s * kStageBytes + 3 * kPlane + p * kShortPlane, &map_s, g.s_rows_inner ? r0 : k0, g.s_rows_inner ? k0 : r0, p, full + 8 * s);
+        for (int p = 0; p < 3; ++p) tma_load<1>(to + kLongBytes + p * kBN * 128, &map_s, k0, ts * kBN, p, full + 8 * s);
       }
       if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
-      // every stage filled is read by the MMAs before the shared memory goes; having given up, what is under way gets its time to land
-      for (long long j = n > kStages ? n - kStages : 0; j < n; ++j)
+      // every stage filled is used up before the shared memory goes; having given up, what is under way gets its time to land
+      for (int j = n > kStages ? n - kStages : 0; j < n; ++j)
         if (!mbar_wait((ok ? empty : full) + 8 * (uint32_t)(j % kStages), (uint32_t)(j / kStages) & 1u, limit)) {
           if (ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
           break;
         }
     }
     __syncwarp();
+  } else if (warp >= kEpiWarps && warp < kEpiWarps + kSplitWarps) {
+    // two groups of four warps, a block each in turn, so that the latencies of one overlap the other's work; a lane per row
+    const int row = (warp & 3) * 32 + lane, group = (warp - kEpiWarps) >> 2;
+    bool ok = true;
+    for (int n = group; n < run; n += 2) {
+      const uint32_t s = (uint32_t)(n % kStages), from = ring + s * Z::kStageBytes;
+      ok = !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kStages) & 1u, limit) &&
+           mbar_wait(aempty + 8 * group, (((uint32_t)n >> 1) & 1u) ^ 1u, limit);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t to = tmem + Z::kA + group * 96 + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t p0[16], p1[16], p2[16];
+        if (g.l_rows_inner) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float x, y;
+            const uint32_t q = from + (uint32_t)((half * 32 + 2 * j) * kRows + row) * 4;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(q) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(q + kRows * 4) : "memory");
+            uint32_t w[3];
+            split_pair(x, y, w);
+            p0[j] = w[0]; p1[j] = w[1]; p2[j] = w[2];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float4 v;
+            const uint32_t q = from + half * (kLongBytes / 2) + row * 128 + ((j ^ (row & 7)) << 4);
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(q) : "memory");
+            uint32_t w[3];
+            split_pair(v.x, v.y, w);
+            p0[2 * j] = w[0]; p1[2 * j] = w[1]; p2[2 * j] = w[2];
+            split_pair(v.z, v.w, w);
+            p0[2 * j + 1] = w[0]; p1[2 * j + 1] = w[1]; p2[2 * j + 1] = w[2];
+          }
+        }
+        __syncwarp();
+        tmem_store16(to + half * 16, p0);
+        tmem_store16(to + half * 16 + 32, p1);
+        tmem_store16(to + half * 16 + 64, p2);
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(afull + 8 * group);
+    }
+    if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
+    __syncwarp();
   } else if (warp == kMmaWarp) {
     if (lane == 0) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)g.l_rows_inner << 15) | ((uint32_t)g.s_rows_inner << 16) |
-                             ((uint32_t)(kBN >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-      const uint32_t adv_a = g.l_rows_inner ? 128 : 2, adv_b = g.s_rows_inner ? 128 : 2;
+      constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24);      // bfloat16, k along memory in B
       bool ok = true;
-      long long n = 0;
       uint32_t v = 0;
-      for (long long u = u0; u < u1 && ok; ++v) {
+      for (int n = 0; n < run && ok; ++v) {
         // a segment: up to kSegment blocks of one tile
-        const int len = (int)min(min((long long)kSegment, u1 - u), g.blocks - u % g.blocks);
+        const int len = min(min(kSegment, run - n), g.blocks - at.block);
         ok = !s_abort && mbar_wait(tempty + 8 * (v & 1u), ((v >> 1) & 1u) ^ 1u, limit);
         if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + (v & 1u) * kBN;
-        for (int i = 0; i < len; ++i, ++n) {
-          const uint32_t s = (uint32_t)(n % kStages);
-          ok = !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kStages) & 1u, limit);
+        const uint32_t d = tmem + (v & 1u) * Z::kD;
+        for (int i = 0; i < len; ++i, ++n, at.next(g)) {
+          const uint32_t s = (uint32_t)(n % kStages), b = n & 1;
+          ok = !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kStages) & 1u, limit) && mbar_wait(afull + 8 * b, ((uint32_t)n >> 1) & 1u, limit);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t at = tiles + s * kStageBytes;
+          const uint64_t db = umma_desc(ring + s * Z::kStageBytes + kLongBytes, false);
+          const uint32_t da = tmem + Z::kA + b * 96;
 #pragma unroll
-          for (int q = 0; q < 6; ++q) {
-            const uint64_t da = umma_desc(at + ((0x201100 >> (4 * (5 - q))) & 3) * kPlane, g.l_rows_inner),
-                           db = umma_desc(at + 3 * kPlane + ((0x021010 >> (4 * (5 - q))) & 3) * kShortPlane, g.s_rows_inner);
-#pragma unroll
-            for (int j = 0; j < kBlockK / 16; ++j)
-              umma<1>(d, da + (uint64_t)(j * adv_a), db + (uint64_t)(j * adv_b), idesc, i > 0 || q > 0 || j > 0);
+          for (int j = 0; j < kBlockK / 16; ++j) {
+            umma_a_tmem(d, da + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(3 * kBN >> 3) << 17), i > 0 || j > 0);
+            umma_a_tmem(d + kBN, da + 32 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(2 * kBN >> 3) << 17), 1);
+            umma_a_tmem(d + 2 * kBN, da + 64 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(kBN >> 3) << 17), 1);
           }
           umma_commit<1>(empty + 8 * s);
+          umma_commit<1>(aempty + 8 * b);
         }
         if (!ok) break;
         umma_commit<1>(tfull + 8 * (v & 1u));
-        u += len;
       }
       if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     }
@@ -199,48 +226,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear_split(const __grid_const
   } else {
     bool ok = true;
     uint32_t v = 0;
-    for (long long u = u0; u < u1 && ok;) {
+    for (int n = 0; n < run && ok;) {
       // a piece: this CTA's blocks of one tile
-      const int t = (int)(u / g.blocks);
-      const long long end = min(u1, (long long)(t + 1) * g.blocks);
-      const bool whole = end - u == g.blocks;
+      const int piece = min(run - n, g.blocks - at.block);
       float acc[kBN];
 #pragma unroll
       for (int j = 0; j < kBN; ++j) acc[j] = 0.f;
-      for (long long k = u; k < end && ok; k += kSegment, ++v) {
+      for (int k = 0; k < piece && ok; k += kSegment, ++v) {
         ok = !s_abort && mbar_wait(tfull + 8 * (v & 1u), (v >> 1) & 1u, limit);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + (v & 1u) * Z::kD + ((uint32_t)(warp * 32) << 16);
 #pragma unroll
         for (int c = 0; c < kBN / 16; ++c) {
-          uint32_t r[16];
-          tmem_load16(tmem + (v & 1u) * kBN + c * 16 + ((uint32_t)(warp * 32) << 16), r);
+          uint32_t r0[16], r1[16], r2[16];
+          tmem_load16(d + c * 16, r0);
+          tmem_load16(d + kBN + c * 16, r1);
+          tmem_load16(d + 2 * kBN + c * 16, r2);
           tmem_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[c * 16 + j] += __uint_as_float(r[j]);
+          for (int j = 0; j < 16; ++j) acc[c * 16 + j] += __uint_as_float(r0[j]) + (__uint_as_float(r1[j]) + __uint_as_float(r2[j]));
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tempty + 8 * (v & 1u)) : "memory");
+        if (lane == 0) mbar_arrive(tempty + 8 * (v & 1u));
       }
       if (!ok) break;
       int tl, ts;
-      tile_of(g, t, &tl, &ts);
+      tile_of(g, at.tile, &tl, &ts);
       const int row = warp * 32 + lane;
       const long long l = (long long)tl * kRows + row;
-      if (whole) {
+      if (piece == g.blocks) {
         if (l < g.nl)
 #pragma unroll
           for (int j = 0; j < kBN; ++j)
             if (ts * kBN + j < g.ns) finish_split(g, acc[j], l, ts * kBN + j);
       } else {
-        float* p = g.partial + ((long long)(2 * blockIdx.x + (u == u0 ? 0 : 1)) * kBN) * kRows + row;
+        float* p = g.partial + ((long long)(2 * blockIdx.x + (n == 0 ? 0 : 1)) * kBN) * kRows + row;
 #pragma unroll
         for (int j = 0; j < kBN; ++j) p[j * kRows] = acc[j];
       }
       __syncwarp();
-      u = end;
+      n += piece;
+      at.block += piece;
+      if (at.block == g.blocks) { at.block = 0; ++at.tile; }
     }
     if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     __syncwarp();
@@ -250,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear_split(const __grid_const
   if (warp == kMmaWarp) {
     __syncwarp();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
 }
 
@@ -280,25 +310,45 @@ __global__ void __launch_bounds__(256) k_linear_split_sum(const __grid_constant_
   }
 }
 
-int width_of(long long ns) { return ns <= 32 ? 32 : 64; }
+// As few tiles along the short side as its width allows (each goes through the long side, the second from L2), the narrower where both make as many.
+int width_of(long long ns) { return (ns + 47) / 48 < (ns + 31) / 32 ? 48 : 32; }
 int ctas_of(long long nl, long long ns, long long nk) {
   const long long units = (nl + kRows - 1) / kRows * ((ns + width_of(ns) - 1) / width_of(ns)) * ((nk + kBlockK - 1) / kBlockK);
   const long long n = (units + 3) / 4;                   // four blocks each at least
   return (int)(n < kMostCtas ? n : kMostCtas);
 }
 
+// The long side as it is: 128 rows of 64 k (rows along memory), or 32 k of 128 rows with the 128-byte swizzle, without which a lane per row would
+// meet bank conflicts (k along memory).
+bool encode_long(CUtensorMap* map, const Operand& L, long long nl, long long nk) {
+  const bool rows_inner = L.ks != 1;
+  const cuuint64_t dims[2] = {(cuuint64_t)(rows_inner ? nl : nk), (cuuint64_t)(rows_inner ? nk : nl)};
+  const long long pitch = dims[1] > 1 ? (rows_inner ? L.ks : L.rs) : (long long)((dims[0] + 3) / 4 * 4);
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch * 4};
+  const cuuint32_t box[2] = {rows_inner ? 128u : 32u, rows_inner ? 64u : 128u}, estr[2] = {1, 1};
+  return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(L.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              rows_inner ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int kBN>
-cudaError_t launch(const Planes& S, const SplitArgs& g, cudaStream_t s) {
-  alignas(64) CUtensorMap map;
+cudaError_t launch(const Operand& L, const Planes& S, long long nk, const SplitArgs& g, cudaStream_t s) {
+  alignas(64) CUtensorMap ml, ms;
   if (tensor_map_encoder() == nullptr) return cudaErrorNotSupported;
-  if (!encode_operand(&map, S, true, kBN)) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(k_linear_split<kBN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
-  if (e == cudaSuccess) e = launch_chained(k_linear_split<kBN>, dim3((unsigned)g.ctas), kThreads, kSmem, s, map, g);
+  if (!encode_long(&ml, L, g.nl, nk) || !encode_operand(&ms, S, true, kBN)) return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(k_linear_split<kBN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sizes<kBN>::kSmem);
+  if (e == cudaSuccess) e = launch_chained(k_linear_split<kBN>, dim3((unsigned)g.ctas), kThreads, Sizes<kBN>::kSmem, s, ml, ms, g);
   if (e == cudaSuccess && g.ctas > 1) e = launch_chained(k_linear_split_sum<kBN>, dim3((unsigned)(g.tiles_l * g.tiles_s)), 256, 0, s, g);
   return e;
 }
 
 }  // namespace
+
+bool linear_split_takes(const Operand& L, long long nl, long long nk) {
+  if (((uintptr_t)L.p & 15) != 0 || (L.rs != 1 && L.ks != 1)) return false;
+  const long long pitch = L.ks != 1 ? L.ks : L.rs, inner = L.ks != 1 ? nl : nk, outer = L.ks != 1 ? nk : nl;
+  return outer == 1 || (pitch % 4 == 0 && pitch >= inner);
+}
 
 size_t linear_split_workspace(long long nl, long long ns, long long nk) {
   return (size_t)2 * ctas_of(nl, ns, nk) * width_of(ns) * kRows * sizeof(float);
@@ -307,18 +357,16 @@ size_t linear_split_workspace(long long nl, long long ns, long long nk) {
 cudaError_t launch_linear_split(const Operand& L, const Planes& S, long long nl, long long ns, long long nk, bool long_is_b, const Finish& f,
                                 void* workspace, unsigned int* status, bool stall, cudaStream_t s) {
   SplitArgs g = {};
-  g.L = L; g.nk = nk; g.nl = (int)nl; g.ns = (int)ns;
+  g.nl = (int)nl; g.ns = (int)ns;
   g.blocks = (int)((nk + kBlockK - 1) / kBlockK);
   g.tiles_l = (int)((nl + kRows - 1) / kRows);
   g.tiles_s = (int)((ns + width_of(ns) - 1) / width_of(ns));
   g.ctas = ctas_of(nl, ns, nk);
-  g.l_rows_inner = L.ks != 1; g.s_rows_inner = S.rows_inner;
-  const long long pitch = g.l_rows_inner ? L.ks : L.rs;
-  g.vec = ((uintptr_t)L.p & 15) == 0 && pitch % 4 == 0;
+  g.l_rows_inner = L.ks != 1;
   g.long_is_b = long_is_b; g.stall = stall;
   g.partial = static_cast<float*>(workspace);
   g.status = status; g.f = f;
-  return width_of(ns) == 32 ? launch<32>(S, g, s) : launch<64>(S, g, s);
+  return width_of(ns) == 32 ? launch<32>(L, S, nk, g, s) : launch<48>(L, S, nk, g, s);
 }
 
 }  // namespace strads

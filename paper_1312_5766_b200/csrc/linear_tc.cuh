@@ -29,8 +29,9 @@ EncodeFn tensor_map_encoder();           // null: the driver has none
 bool encode_operand(CUtensorMap* map, const Planes& m, bool bf16, int box_rows);
 
 // ---- binary32 products with up to kSplitMost rows on one side (linear_split.cu) ----
-// The long side L (rs or ks 1) is read where it is and split into planes on its way to shared memory; the short one comes as planes.
+// The long side L is read where it is, if linear_split_takes it, and split into planes on its way; the short one comes as planes, k along memory.
 constexpr int kSplitMost = 128;
+bool linear_split_takes(const Operand& L, long long nl, long long nk);
 size_t linear_split_workspace(long long nl, long long ns, long long nk);      // (the same on every device)
 cudaError_t launch_linear_split(const Operand& L, const Planes& S, long long nl, long long ns, long long nk, bool long_is_b, const Finish& f,
                                 void* workspace, unsigned int* status, bool stall, cudaStream_t s);

@@ -6,7 +6,8 @@
 //   rows along memory (k_thin_rows): a lane takes the rows of 16 bytes (or of 4, where there are few), a warp every 16th k; warps
 //   are added through shared memory.
 //
-// What hides the memory's latency is the number of loads under way: eight per lane, and enough warps; where the rows alone do not
+// What hides the memory's latency is the number of loads under way: four or eight per lane, and as many warps as that leaves registers for (rows along
+// memory, 10,000 x 100,000 binary32: 767 us with 4 a lane, 833 with 8, 2,280 with 16 and half the warps); where the rows alone do not
 // make enough of them, the warps of a CTA and the CTAs of a cluster share k and add through (distributed) shared memory, in a fixed order.
 // The short side is staged in shared memory as binary32, or (k along memory, up to four rows) read through L1 as it is.
 #include <mutex>
@@ -200,10 +201,10 @@ __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thi
 constexpr int kRowWarps = 16, kRowThreads = 32 * kRowWarps;
 template <typename T, int kT, int kBytes>
 __global__ void __launch_bounds__(kRowThreads) k_thin_rows(const __grid_constant__ Thin t) {
-  constexpr int kV = kBytes / sizeof(T), kTile = 32 * kV, kStage = kStageFloats / kT, kU = 8;
-  __shared__ __align__(16) float sh[kStageFloats];
-  float* sum = sh;                                       // [kT][kTile], when the last of the short side has been used
-  static_assert(kT * kTile <= kStageFloats, "the sums take the stage's place");
+  constexpr int kV = kBytes / sizeof(T), kTile = 32 * kV, kStage = kStageFloats / kT, kU = sizeof(T) == 2 && kT == 1 ? 8 : 4;
+  constexpr int kSums = kT * kTile;
+  extern __shared__ __align__(16) float sh[];            // the stage; when the last of the short side has been used, [warp][kSums]
+  __shared__ float sum[kSums];
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long l0 = (long long)(blockIdx.x / t.splits) * kTile, l = l0 + lane * kV;
@@ -247,16 +248,17 @@ __global__ void __launch_bounds__(kRowThreads) k_thin_rows(const __grid_constant
       }
     }
   }
-  for (int w = 0; w < kRowWarps; ++w) {                  // in the order of the warps
-    __syncthreads();
-    if (warp == w)
+  __syncthreads();
 #pragma unroll
-      for (int s = 0; s < kT; ++s)
+  for (int s = 0; s < kT; ++s)
 #pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          float* p = sum + s * kTile + v * 32 + lane;      // (a lane's rows 32 apart: no bank conflicts)
-          *p = w == 0 ? acc[s][v] : *p + acc[s][v];
-        }
+    for (int v = 0; v < kV; ++v) sh[warp * kSums + s * kTile + v * 32 + lane] = acc[s][v];      // (a lane's rows 32 apart: no bank conflicts)
+  __syncthreads();
+  for (int i = threadIdx.x; i < kSums; i += kRowThreads) {
+    float a = sh[i];
+#pragma unroll
+    for (int w = 1; w < kRowWarps; ++w) a += sh[w * kSums + i];
+    sum[i] = a;
   }
   if (t.splits > 1) cluster_sync(); else __syncthreads();
   const int rank = t.splits > 1 ? (int)(blockIdx.x % t.splits) : 0;
@@ -280,7 +282,12 @@ cudaError_t launch_rows(const Thin& t, long long tiles, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(k_thin_rows<T, kT, kBytes>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
   }
-  return launch_chained_cluster(k_thin_rows<T, kT, kBytes>, dim3((unsigned)(tiles * t.splits)), kRowThreads, 0, s, t.splits, t);
+  constexpr size_t kSums = sizeof(float) * kRowWarps * kT * 32 * (kBytes / sizeof(T)), kStage = sizeof(float) * kStageFloats, kSmem = kSums > kStage ? kSums : kStage;
+  if (kSmem + 8192 > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(k_thin_rows<T, kT, kBytes>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_chained_cluster(k_thin_rows<T, kT, kBytes>, dim3((unsigned)(tiles * t.splits)), kRowThreads, kSmem, s, t.splits, t);
 }
 template <typename T, int kT>
 cudaError_t launch(Thin t, int sms, cudaStream_t s) {
@@ -301,7 +308,7 @@ cudaError_t launch(Thin t, int sms, cudaStream_t s) {
   t.vec = vec_ok(t.L.p, t.L.ks, t.nk, sizeof(T));
   // 16 bytes of a row per lane where that leaves enough CTAs, 4 otherwise; then as many CTAs to a tile as keep four on every SM
   const long long wide = (t.nl + 512 / (int)sizeof(T) - 1) / (512 / (int)sizeof(T)), narrow = (t.nl + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T));
-  const bool few = wide * 16 < 2ll * sms;
+  const bool few = wide * 32 < sms;
   const long long tiles = few ? narrow : wide;
   while (t.splits < 16 && tiles * t.splits < 4ll * sms && t.nk >= 512ll * t.splits) t.splits *= 2;
   return few ? launch_rows<T, kT, 4>(t, tiles, s) : launch_rows<T, kT, 16>(t, tiles, s);
