@@ -26,10 +26,11 @@ __global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long lon
 #pragma unroll
       for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(x)[j] = __ldg(reinterpret_cast<const uint4*>(at) + j);
     } else {
+      const long long last = inner - 1 - k;              // (< 0: a group of padding alone; clamped, not branched: all loads under way at once)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) if (k + j < inner) x[j] = at[j * inner_stride];
+      for (int j = 0; j < 8; ++j) x[j] = at[(j < last ? j : last) * inner_stride];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) if (k + j >= inner) store_f32(&x[j], 0.f);
+      for (int j = 0; j < 8; ++j) if (j > last) store_f32(&x[j], 0.f);
     }
     unsigned short* to = dst + o * ld + k;
     if (sizeof(T) == 2) {
@@ -49,8 +50,53 @@ __global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long lon
 }
 
 // ---- gz = scale gout act'(preact), and its column sums ----
-// A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row.  gz (may be null) [n][ld], rounded to T;
-// partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
+// A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row, kU of them at a time so that their loads are under way
+// together.  gz (may be null) [n][ld], rounded to T; partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
+template <typename T, bool kVec>
+__device__ __forceinline__ void load8(const T* p, long long stride, int count, T (&x)[8]) {
+  if (kVec) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(x)[j] = __ldg(reinterpret_cast<const uint4*>(p) + j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = p[min(j, count - 1) * stride];
+  }
+}
+template <typename T, bool kVec>
+__device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, int act, float scale, T* gz, long long ld, long long c, long long r0,
+                                        long long r1, int warp, float (&total)[8]) {
+  constexpr int kU = 4;
+  const int count = (int)min(8ll, m - c);
+  for (long long r = r0 + warp; r < r1; r += 8 * kU) {
+    __align__(16) T g[kU][8], z[kU][8];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const long long row = min(r + 8 * u, r1 - 1);
+      load8<T, kVec>(static_cast<const T*>(gout.p) + row * gout.rs + c * gout.ks, gout.ks, count, g[u]);
+      if (act != STRADS_ACT_IDENTITY) load8<T, kVec>(static_cast<const T*>(preact.p) + row * preact.rs + c * preact.ks, preact.ks, count, z[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      if (r + 8 * u >= r1) break;
+      __align__(16) T out[8];
+      float v[8], zf[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = j < count ? scale * load_f32(&g[u][j]) : 0.f;
+        zf[j] = act != STRADS_ACT_IDENTITY ? load_f32(&z[u][j]) : 0.f;
+      }
+      times_slope<sizeof(T) == 4>(zf, v, act);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j < count) total[j] += v[j];
+        store_f32(&out[j], v[j]);
+      }
+      if (gz != nullptr)                                 // (ld is a multiple of 8: the last group has its place)
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(gz + (r + 8 * u) * ld + c)[j] = reinterpret_cast<const uint4*>(out)[j];
+    }
+  }
+}
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand preact, long long n, long long m, int act, float scale, T* gz, long long ld,
                                                         float* partial, long long rows, int vec) {
@@ -59,44 +105,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand pr
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
   float total[8] = {};
-  for (long long r = r0 + warp; r < r1; r += 8) {
-    __align__(16) T g[8], z[8];
-    const T *gp = static_cast<const T*>(gout.p) + r * gout.rs + c * gout.ks, *zp = static_cast<const T*>(preact.p) + r * preact.rs + c * preact.ks;
-    if (vec && c + 8 <= m) {
-#pragma unroll
-      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(g)[j] = __ldg(reinterpret_cast<const uint4*>(gp) + j);
-      if (act != STRADS_ACT_IDENTITY)
-#pragma unroll
-        for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(z)[j] = __ldg(reinterpret_cast<const uint4*>(zp) + j);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        store_f32(&g[j], 0.f);
-        store_f32(&z[j], 0.f);
-        if (c + j < m) {
-          g[j] = gp[j * gout.ks];
-          if (act != STRADS_ACT_IDENTITY) z[j] = zp[j * preact.ks];
-        }
-      }
-    }
-    __align__(16) T out[8];
-    float v[8], zf[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = scale * load_f32(&g[j]);
-      zf[j] = act != STRADS_ACT_IDENTITY ? load_f32(&z[j]) : 0.f;
-    }
-    times_slope<sizeof(T) == 4>(zf, v, act);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      total[j] += v[j];
-      store_f32(&out[j], v[j]);
-    }
-    if (gz != nullptr && c < m) {                        // (ld is a multiple of 8: the last group has its place)
-#pragma unroll
-      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(gz + r * ld + c)[j] = reinterpret_cast<const uint4*>(out)[j];
-    }
-  }
+  if (vec && c + 8 <= m) gz_rows<T, true>(gout, preact, m, act, scale, gz, ld, c, r0, r1, warp, total);
+  else if (c < m) gz_rows<T, false>(gout, preact, m, act, scale, gz, ld, c, r0, r1, warp, total);
   if (partial == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[warp][j * 33 + lane] = total[j];
@@ -109,15 +119,24 @@ __global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand pr
     partial[(long long)blockIdx.y * m + col] = v;
   }
 }
+// 32 columns to a CTA, eight warps taking a run of the blocks of rows each.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_linear_bias_grad(const float* partial, int blocks, long long m, T* gbias) {
+  __shared__ float sum[8][32];
   chain_begin();
-  const long long c = (long long)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= m) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 32 + lane;
   float s = 0.f;
-#pragma unroll 8
-  for (int r = 0; r < blocks; ++r) s += partial[r * m + c];
-  store_f32(gbias + c, s);
+  if (c < m)
+#pragma unroll 4
+    for (int r = blocks * warp / 8; r < blocks * (warp + 1) / 8; ++r) s += partial[r * m + c];
+  sum[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < m) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += sum[w][lane];
+    store_f32(gbias + c, s);
+  }
 }
 
 template <typename T>
@@ -263,7 +282,7 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
   c.err = launch_chained(k_linear_gz<T>, dim3((unsigned)((g.n_out + 255) / 256), (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
                          (int)g.activation, g.scale, gz, ld, partial, rows, vec);
   if (gbias != nullptr && c.err == cudaSuccess)
-    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + kThreads - 1) / kThreads)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, gbias);
+    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, gbias);
 }
 
 template <typename T>

@@ -121,20 +121,46 @@ __device__ __forceinline__ void times_slope(const float (&z)[kN], float (&v)[kN]
   }
 }
 
-// One element of D.
+// kN elements of D in a row, `step` apart along b: a, b + j step, of which the first `count` (at least one) exist.  `here`: row a exists (else
+// a is one that does, and nothing is stored).  Loads go to clamped places without a branch, so that they are all under way at
+// once, and come before the stores: out may be the residual.
+template <typename T, int kN>
+__device__ __forceinline__ void finish_run(const Finish& f, float (&v)[kN], long long a, long long b, long long step, int count, bool here) {
+  const long long sb_out = step * f.out.sb;
+  T* out = static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + b * f.out.sb;
+  if (!f.plain) {
+    float r[kN];
+    if (f.residual.p) {
+      const T* p = static_cast<const T*>(f.residual.p) + a * f.residual.sa + b * f.residual.sb;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) r[j] = load_f32(p + min(j, count - 1) * (step * f.residual.sb));
+    }
+    if (f.bias) {
+      const T* p = static_cast<const T*>(f.bias) + a * f.bias_a + b * f.bias_b;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] += load_f32(p + min(j, count - 1) * (step * f.bias_b));
+    }
+    if (f.preact.p) {
+      T* p = static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + b * f.preact.sb;
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+        if (here && j < count) store_f32(p + j * (step * f.preact.sb), v[j]);
+    }
+    activate_all<sizeof(T) == 4>(v, f.act);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] = f.residual.p ? fmaf(f.scale, v[j], r[j]) : f.scale * v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] *= f.scale;
+  }
+#pragma unroll
+  for (int j = 0; j < kN; ++j)
+    if (here && j < count) store_f32(out + j * sb_out, v[j]);
+}
 template <typename T>
 __device__ __forceinline__ void finish(const Finish& f, float z, long long a, long long b) {
-  if (f.plain) {
-    z *= f.scale;
-  } else {
-    if (f.bias) z += load_f32(static_cast<const T*>(f.bias) + a * f.bias_a + b * f.bias_b);
-    if (f.preact.p) store_f32(static_cast<T*>(const_cast<void*>(f.preact.p)) + a * f.preact.sa + b * f.preact.sb, z);
-    float v[1] = {z};
-    activate_all<sizeof(T) == 4>(v, f.act);
-    z = f.scale * v[0];
-    if (f.residual.p) z += load_f32(static_cast<const T*>(f.residual.p) + a * f.residual.sa + b * f.residual.sb);
-  }
-  store_f32(static_cast<T*>(const_cast<void*>(f.out.p)) + a * f.out.sa + b * f.out.sb, z);
+  float v[1] = {z};
+  finish_run<T, 1>(f, v, a, b, 1, 1, true);
 }
 
 // ---- products with few rows on one side (linear_thin.cu) ----

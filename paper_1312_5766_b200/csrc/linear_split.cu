@@ -46,8 +46,22 @@ struct SplitArgs {
 __device__ __forceinline__ long long start_of(const SplitArgs& g, int c) { return (long long)g.tiles_l * g.tiles_s * g.blocks * c / g.ctas; }
 // Tiles of one part of the long side follow each other: the second finds it in L2.
 __device__ __forceinline__ void tile_of(const SplitArgs& g, int t, int* tl, int* ts) { *tl = t / g.tiles_s; *ts = t % g.tiles_s; }
-__device__ __forceinline__ void finish_split(const SplitArgs& g, float v, long long l, long long s) {
-  if (g.long_is_b) finish<float>(g.f, v, s, l); else finish<float>(g.f, v, l, s);
+// Columns s, s + 1, .. of row l (clamped to one that exists; `here`: it does).
+template <int kN>
+__device__ __forceinline__ void finish_split(const SplitArgs& g, float (&v)[kN], long long l, int s) {
+  const bool here = l < g.nl;
+  const long long at = here ? l : g.nl - 1;
+  const int count = min(kN, g.ns - s);
+  if (!g.long_is_b) {
+    finish_run<float, kN>(g.f, v, at, s, 1, count, here);
+  } else {                                               // (the short side is D's a: its strides change places)
+    Finish f = g.f;
+    f.out = {g.f.out.p, g.f.out.sb, g.f.out.sa};
+    f.residual = {g.f.residual.p, g.f.residual.sb, g.f.residual.sa};
+    f.preact = {g.f.preact.p, g.f.preact.sb, g.f.preact.sa};
+    f.bias_a = g.f.bias_b; f.bias_b = g.f.bias_a;
+    finish_run<float, kN>(f, v, at, s, 1, count, here);
+  }
 }
 // Counts through the blocks of a run: tile and block of k.
 struct Walk {
@@ -258,10 +272,13 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
       const int row = warp * 32 + lane;
       const long long l = (long long)tl * kRows + row;
       if (piece == g.blocks) {
-        if (l < g.nl)
 #pragma unroll
-          for (int j = 0; j < kBN; ++j)
-            if (ts * kBN + j < g.ns) finish_split(g, acc[j], l, ts * kBN + j);
+        for (int c = 0; c < kBN; c += 16) {
+          float z[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) z[j] = acc[c + j];
+          if (ts * kBN + c < g.ns) finish_split<16>(g, z, l, ts * kBN + c);
+        }
       } else {
         float* p = g.partial + ((long long)(2 * blockIdx.x + (n == 0 ? 0 : 1)) * kBN) * kRows + row;
 #pragma unroll
@@ -284,30 +301,38 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   }
 }
 
-// Tiles that fell to more than one CTA: a CTA each, adding in the order of the CTAs.
+// Tiles that fell to more than one CTA, eight columns to a CTA, adding in the order of the CTAs.
 template <int kBN>
 __global__ void __launch_bounds__(256) k_linear_split_sum(const __grid_constant__ SplitArgs g) {
   chain_begin();
+  __shared__ int s_first, s_last;
+  __shared__ bool s_begins;                              // the first of the tile's CTAs begins with it (else with the tile before)
   const int t = blockIdx.x;
-  const long long b0 = (long long)t * g.blocks, b1 = b0 + g.blocks;
-  // the CTA that holds the tile's first block: near b0 ctas / (all blocks)
-  int c0 = (int)(b0 * g.ctas / ((long long)g.tiles_l * g.tiles_s * g.blocks));
-  while (c0 + 1 < g.ctas && start_of(g, c0 + 1) <= b0) ++c0;
-  while (c0 > 0 && start_of(g, c0) > b0) --c0;
-  if (start_of(g, c0 + 1) >= b1) return;                 // one CTA had all of it and has finished it
+  if (threadIdx.x == 0) {
+    const long long b0 = (long long)t * g.blocks, b1 = b0 + g.blocks;
+    // the CTA that holds the tile's first block: near b0 ctas / (all blocks)
+    int c = (int)(b0 * g.ctas / ((long long)g.tiles_l * g.tiles_s * g.blocks));
+    while (c + 1 < g.ctas && start_of(g, c + 1) <= b0) ++c;
+    while (c > 0 && start_of(g, c) > b0) --c;
+    s_first = c;
+    s_begins = start_of(g, c) == b0;
+    while (c + 1 < g.ctas && start_of(g, c + 1) < b1) ++c;
+    s_last = c;
+  }
+  __syncthreads();
+  const int c0 = s_first, c1 = s_last;
+  if (c0 == c1) return;                                  // one CTA had all of it and has finished it
   int tl, ts;
   tile_of(g, t, &tl, &ts);
-  for (int i = threadIdx.x; i < kBN * kRows; i += 256) {
-    const int col = i / kRows, row = i % kRows;
-    const long long l = (long long)tl * kRows + row, s = (long long)ts * kBN + col;
-    if (l >= g.nl || s >= g.ns) continue;
-    float v = 0.f;
-    for (int c = c0; c < g.ctas && start_of(g, c) < b1; ++c) {
-      const int slot = 2 * c + (start_of(g, c) >= b0 || start_of(g, c) / g.blocks == t ? 0 : 1);
-      v += g.partial[((long long)slot * kBN + col) * kRows + row];
-    }
-    finish_split(g, v, l, s);
+  const int row = threadIdx.x & (kRows - 1), col = blockIdx.y * 8 + (threadIdx.x >> 7) * 4;
+  if (ts * kBN + col >= g.ns) return;
+  float v[4] = {};
+  for (int c = c0; c <= c1; ++c) {
+    const float* p = g.partial + ((long long)(2 * c + (c > c0 || s_begins ? 0 : 1)) * kBN + col) * kRows + row;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] += p[j * kRows];
   }
+  finish_split<4>(g, v, (long long)tl * kRows + row, ts * kBN + col);
 }
 
 // As few tiles along the short side as its width allows (each goes through the long side, the second from L2), the narrower where both make as many.
@@ -338,7 +363,7 @@ cudaError_t launch(const Operand& L, const Planes& S, long long nk, const SplitA
   if (!encode_long(&ml, L, g.nl, nk) || !encode_operand(&ms, S, true, kBN)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(k_linear_split<kBN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sizes<kBN>::kSmem);
   if (e == cudaSuccess) e = launch_chained(k_linear_split<kBN>, dim3((unsigned)g.ctas), kThreads, Sizes<kBN>::kSmem, s, ml, ms, g);
-  if (e == cudaSuccess && g.ctas > 1) e = launch_chained(k_linear_split_sum<kBN>, dim3((unsigned)(g.tiles_l * g.tiles_s)), 256, 0, s, g);
+  if (e == cudaSuccess && g.ctas > 1) e = launch_chained(k_linear_split_sum<kBN>, dim3((unsigned)(g.tiles_l * g.tiles_s), kBN / 8), 256, 0, s, g);
   return e;
 }
 

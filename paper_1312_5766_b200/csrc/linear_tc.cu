@@ -115,6 +115,10 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
   const long long a = a0 + lane;
   const bool here = a < g.na;
   const uint32_t mine = (uint32_t)lane * sizeof(T);
+  if (!g.out_tma && !g.residual_tma && !g.preact_tma) {
+    finish_run<T, kC>(f, v, here ? a : g.na - 1, b0, 1, min(kC, g.nb - b0), here);
+    return true;
+  }
   float r[kC];
   if (!f.plain) {
     if (g.residual_tma) {
@@ -125,17 +129,16 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
       ++e.got;
       __syncwarp();
     } else if (f.residual.p) {
+      const T* p = static_cast<const T*>(f.residual.p) + (here ? a : g.na - 1) * f.residual.sa + b0 * f.residual.sb;
 #pragma unroll
-      for (int j = 0; j < kC; ++j)
-        r[j] = here && b0 + j < g.nb ? load_f32(static_cast<const T*>(f.residual.p) + a * f.residual.sa + (b0 + j) * f.residual.sb) : 0.f;
+      for (int j = 0; j < kC; ++j) r[j] = load_f32(p + min(j, g.nb - 1 - b0) * f.residual.sb);
     }
     if (f.bias_b == 0) {
 #pragma unroll
       for (int j = 0; j < kC; ++j) v[j] += bias;
     } else if (f.bias) {
 #pragma unroll
-      for (int j = 0; j < kC; ++j)
-        if (b0 + j < g.nb) v[j] += load_f32(static_cast<const T*>(f.bias) + (b0 + j));
+      for (int j = 0; j < kC; ++j) v[j] += load_f32(static_cast<const T*>(f.bias) + min(b0 + j, g.nb - 1));
     }
     if (g.preact_tma) {
       const uint32_t slot = e.out + (e.put++ & 1u) * 2048;
@@ -429,16 +432,24 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       const Item w = item_of(g, first, split);
       const int row = threadIdx.x & (kRows - 1);
       const long long a = (long long)w.ta * kRows + row;
-      for (int col = split * 2 + (int)(threadIdx.x >> 7); col < kBN; col += 2 * g.splits) {
-        const long long b = (long long)w.tb * kBN + col;
-        if (a >= g.na || b >= g.nb) continue;
-        float z = 0.f;
+      // a thread's columns: col, col + step, .., eight at a time
+      constexpr int kN = 8;
+      const int step = 2 * g.splits, end = min(kBN, g.nb - w.tb * kBN);
+      for (int col = split * 2 + (int)(threadIdx.x >> 7); col < end; col += kN * step) {
+        const int count = min(kN, (end - col + step - 1) / step);
+        float z[kN];
+#pragma unroll
+        for (int j = 0; j < kN; ++j) z[j] = 0.f;
         for (int sp = 0; sp < g.splits; ++sp) {
-          float v;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(mapa(tiles + (uint32_t)((col * kRows + row) * 4), (uint32_t)sp)) : "memory");
-          z += v;
+          const uint32_t peer = mapa(tiles, (uint32_t)sp);
+#pragma unroll
+          for (int j = 0; j < kN; ++j) {
+            float v;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer + (uint32_t)(((col + min(j, count - 1) * step) * kRows + row) * 4)) : "memory");
+            z[j] += v;
+          }
         }
-        finish<T>(g.f, z, a, b);
+        finish_run<T, kN>(g.f, z, a < g.na ? a : g.na - 1, (long long)w.tb * kBN + col, step, count, a < g.na);
       }
     }
   }
