@@ -112,10 +112,26 @@ __device__ __forceinline__ bool finite(float mag) { return mag <= 3.402823466e38
 __device__ __forceinline__ float warp_max(float mag) {                                      // magnitudes order like their bits
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mag)));
 }
-__device__ __forceinline__ float decode_m(int q, float s) {
-  return q == -128 ? __uint_as_float(0x7fc00000u) : __fmul_rn((float)(q * abs(q)), s);
+// Between codes and floats by the sum with 2^23 or 1.5 2^23, whose last bits then are the integer: the conversion instructions go through the
+// unit that the roots and quotients need, at a quarter of the rate.
+constexpr float kUnsigned = 8388608.f, kRounded = 12582912.f;
+__device__ __forceinline__ float decode_m(unsigned int byte, float s) {      // byte: the code as stored, -128 .. 127
+  const float q = __fsub_rn(__uint_as_float(0x4b000000u | (byte ^ 0x80u)), kUnsigned + 128.f);
+  return byte == 0x80u ? __uint_as_float(0x7fc00000u) : __fmul_rn(__fmul_rn(q, fabsf(q)), s);
 }
-__device__ __forceinline__ float decode_root(int q, float s) { return q == 255 ? __uint_as_float(0x7fc00000u) : __fmul_rn((float)(q * q), s); }
+__device__ __forceinline__ float decode_root(unsigned int byte, float s) {
+  const float q = __fsub_rn(__uint_as_float(0x4b000000u | byte), kUnsigned);
+  return byte == 255u ? __uint_as_float(0x7fc00000u) : __fmul_rn(__fmul_rn(q, q), s);
+}
+// The integer nearest to the correctly rounded root of x (ties to even), x <= 2^16, in the last bits.  The approximate root is good to 2^-14
+// there; only where it lies within 2^-12 of the middle between two integers is the exact one needed.
+__device__ __forceinline__ unsigned int nearest_root(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  float t = __fadd_rn(r, kRounded);
+  if (fabsf(fabsf(r - (t - kRounded)) - 0.5f) < 0.000244140625f) t = __fadd_rn(__fsqrt_rn(x), kRounded);
+  return __float_as_uint(t);
+}
 
 // The scale of a block whose largest finite magnitude is `top`, and its inverse (both 0 where the block is stored as noughts).
 __device__ __forceinline__ float scale_of(float top, float inverse_of_largest_code_squared, float* inverse) {
@@ -164,9 +180,9 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tabl
     load8(static_cast<const float*>(e.m) + at, n, vec, lane, m);
     load8(static_cast<const float*>(e.v) + at, n, vec, lane, v);
   } else {
-    int q[8];
+    unsigned int q[8];
     const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
-    load8(static_cast<const signed char*>(e.m) + at, n, vec, lane, q);
+    load8(static_cast<const unsigned char*>(e.m) + at, n, vec, lane, q);
 #pragma unroll
     for (int j = 0; j < 8; ++j) m[j] = decode_m(q[j], s1);
     load8(static_cast<const unsigned char*>(e.v) + at, n, vec, lane, q);
@@ -209,17 +225,15 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tabl
   }
   float r1, r2;
   const float s1 = scale_of(warp_max(top1), 1.f / 16129.f, &r1), s2 = scale_of(warp_max(top2), 1.f / 64516.f, &r2);
-  signed char q1[8];
-  unsigned char q2[8];
+  unsigned char q1[8], q2[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float a = fabsf(m[j]);
-    const int q = __float2int_rn(__fsqrt_rn(__fmul_rn(a, r1)));
-    q1[j] = (signed char)(finite(a) ? (m[j] < 0.f ? -q : q) : -128);
-    const int w = __float2int_rn(__fsqrt_rn(__fmul_rn(root[j], r2)));
-    q2[j] = (unsigned char)(finite(root[j]) ? (root[j] > 0.f ? max(w, 1) : w) : 255);
+    const unsigned int q = nearest_root(__fmul_rn(a, r1)), w = nearest_root(__fmul_rn(root[j], r2));
+    q1[j] = (unsigned char)(finite(a) ? (m[j] < 0.f ? 0u - q : q) : 0x80u);
+    q2[j] = (unsigned char)(finite(root[j]) ? (root[j] > 0.f && (w & 0xffu) == 0u ? 1u : w) : 255u);
   }
-  store8(static_cast<signed char*>(e.m) + at, n, vec, lane, q1);
+  store8(static_cast<unsigned char*>(e.m) + at, n, vec, lane, q1);
   store8(static_cast<unsigned char*>(e.v) + at, n, vec, lane, q2);
   if (lane == 0) { e.m_scale[at / kBlock] = s1; e.v_scale[at / kBlock] = s2; }
 }
@@ -235,8 +249,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw_unpack(const __grid_constant
   if (at >= n_all) return;
   const int n = (int)min((long long)kBlock, n_all - at);
   const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
-  int q1[8], q2[8];
-  load8(static_cast<const signed char*>(e.m) + at, n, vec, lane, q1);
+  unsigned int q1[8], q2[8];
+  load8(static_cast<const unsigned char*>(e.m) + at, n, vec, lane, q1);
   load8(static_cast<const unsigned char*>(e.v) + at, n, vec, lane, q2);
   float m[8], v[8];
 #pragma unroll

@@ -62,10 +62,10 @@ __device__ __forceinline__ void load8(const T* p, long long stride, int count, T
     for (int j = 0; j < 8; ++j) x[j] = p[min(j, count - 1) * stride];
   }
 }
-template <typename T, bool kVec>
-__device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, int act, float scale, T* gz, long long ld, long long c, long long r0,
+template <typename T, int kAct, bool kVec>
+__device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, float scale, T* gz, long long ld, long long c, long long r0,
                                         long long r1, int warp, float (&total)[8]) {
-  constexpr int kU = 4;
+  constexpr int kU = kAct == STRADS_ACT_IDENTITY || sizeof(T) == 2 ? 4 : 2;
   const int count = (int)min(8ll, m - c);
   for (long long r = r0 + warp; r < r1; r += 8 * kU) {
     __align__(16) T g[kU][8], z[kU][8];
@@ -73,23 +73,18 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
     for (int u = 0; u < kU; ++u) {
       const long long row = min(r + 8 * u, r1 - 1);
       load8<T, kVec>(static_cast<const T*>(gout.p) + row * gout.rs + c * gout.ks, gout.ks, count, g[u]);
-      if (act != STRADS_ACT_IDENTITY) load8<T, kVec>(static_cast<const T*>(preact.p) + row * preact.rs + c * preact.ks, preact.ks, count, z[u]);
+      if (kAct != STRADS_ACT_IDENTITY) load8<T, kVec>(static_cast<const T*>(preact.p) + row * preact.rs + c * preact.ks, preact.ks, count, z[u]);
     }
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       if (r + 8 * u >= r1) break;
       __align__(16) T out[8];
-      float v[8], zf[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[j] = j < count ? scale * load_f32(&g[u][j]) : 0.f;
-        zf[j] = act != STRADS_ACT_IDENTITY ? load_f32(&z[u][j]) : 0.f;
-      }
-      times_slope<sizeof(T) == 4>(zf, v, act);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j < count) total[j] += v[j];
-        store_f32(&out[j], v[j]);
+        float v = scale * load_f32(&g[u][j]);
+        if (kAct != STRADS_ACT_IDENTITY) v *= slope_as<sizeof(T) == 4, kAct>(load_f32(&z[u][j]));
+        if (kVec || j < count) total[j] += v;
+        store_f32(&out[j], v);
       }
       if (gz != nullptr)                                 // (ld is a multiple of 8: the last group has its place)
 #pragma unroll
@@ -97,16 +92,16 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
     }
   }
 }
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand preact, long long n, long long m, int act, float scale, T* gz, long long ld,
+template <typename T, int kAct>
+__global__ void __launch_bounds__(kThreads) k_linear_gz(Operand gout, Operand preact, long long n, long long m, float scale, T* gz, long long ld,
                                                         float* partial, long long rows, int vec) {
   __shared__ float sum[8][256 + 8];
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
   float total[8] = {};
-  if (vec && c + 8 <= m) gz_rows<T, true>(gout, preact, m, act, scale, gz, ld, c, r0, r1, warp, total);
-  else if (c < m) gz_rows<T, false>(gout, preact, m, act, scale, gz, ld, c, r0, r1, warp, total);
+  if (vec && c + 8 <= m) gz_rows<T, kAct, true>(gout, preact, m, scale, gz, ld, c, r0, r1, warp, total);
+  else if (c < m) gz_rows<T, kAct, false>(gout, preact, m, scale, gz, ld, c, r0, r1, warp, total);
   if (partial == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[warp][j * 33 + lane] = total[j];
@@ -269,8 +264,12 @@ void forward(Call& c, const strads_linear_config_t& g, const void* bias, const s
 
 template <typename T>
 void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, T* gz, long long ld, T* gbias) {
-  long long rows = (g.n_rows + 127) / 128;                              // at most 128 blocks of rows, of at least 64 and a multiple of 8
-  rows = rows < 64 ? 64 : (rows + 7) / 8 * 8;
+  // at most 128 blocks of rows; of 64 rows where that leaves four CTAs to an SM, else of as few as 8
+  const long long columns = (g.n_out + 255) / 256;
+  long long rows = (g.n_rows * columns + 4 * 148 - 1) / (4 * 148);
+  if (rows > 64) rows = 64;
+  if (rows * 128 < g.n_rows) rows = (g.n_rows + 127) / 128;
+  rows = (rows + 7) / 8 * 8;
   const int blocks = (int)((g.n_rows + rows - 1) / rows);
   float* partial = gbias != nullptr || !c.run ? static_cast<float*>(c.take((size_t)blocks * (size_t)g.n_out * sizeof(float))) : nullptr;
   if (!c.run || c.err != cudaSuccess) return;
@@ -279,8 +278,17 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
   if (preact) z = operand_of(*preact);
   const int vec = gout.col_stride == 1 && vec_rows(gout.data, gout.row_stride, g.n_rows, sizeof(T)) &&
                   (g.activation == STRADS_ACT_IDENTITY || (z.ks == 1 && vec_rows(z.p, z.rs, g.n_rows, sizeof(T))));
-  c.err = launch_chained(k_linear_gz<T>, dim3((unsigned)((g.n_out + 255) / 256), (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
-                         (int)g.activation, g.scale, gz, ld, partial, rows, vec);
+  void (*kernel)(Operand, Operand, long long, long long, float, T*, long long, float*, long long, int) = k_linear_gz<T, STRADS_ACT_IDENTITY>;
+  switch (g.activation) {
+    case STRADS_ACT_RELU: kernel = k_linear_gz<T, STRADS_ACT_RELU>; break;
+    case STRADS_ACT_SIGMOID: kernel = k_linear_gz<T, STRADS_ACT_SIGMOID>; break;
+    case STRADS_ACT_GELU: kernel = k_linear_gz<T, STRADS_ACT_GELU>; break;
+    case STRADS_ACT_GELU_TANH: kernel = k_linear_gz<T, STRADS_ACT_GELU_TANH>; break;
+    case STRADS_ACT_SILU: kernel = k_linear_gz<T, STRADS_ACT_SILU>; break;
+    default: break;
+  }
+  c.err = launch_chained(kernel, dim3((unsigned)columns, (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
+                         g.scale, gz, ld, partial, rows, vec);
   if (gbias != nullptr && c.err == cudaSuccess)
     c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, gbias);
 }

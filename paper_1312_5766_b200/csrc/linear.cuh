@@ -104,23 +104,6 @@ __device__ __forceinline__ void activate_all(float (&v)[kN], int act) {
     default: break;
   }
 }
-template <bool kExact, int kAct, int kN>
-__device__ __forceinline__ void slope_run(const float (&z)[kN], float (&v)[kN]) {
-#pragma unroll
-  for (int j = 0; j < kN; ++j) v[j] *= slope_as<kExact, kAct>(z[j]);
-}
-template <bool kExact, int kN>
-__device__ __forceinline__ void times_slope(const float (&z)[kN], float (&v)[kN], int act) {      // v *= act'(z)
-  switch (act) {
-    case STRADS_ACT_RELU: slope_run<kExact, STRADS_ACT_RELU>(z, v); break;
-    case STRADS_ACT_SIGMOID: slope_run<kExact, STRADS_ACT_SIGMOID>(z, v); break;
-    case STRADS_ACT_GELU: slope_run<kExact, STRADS_ACT_GELU>(z, v); break;
-    case STRADS_ACT_GELU_TANH: slope_run<kExact, STRADS_ACT_GELU_TANH>(z, v); break;
-    case STRADS_ACT_SILU: slope_run<kExact, STRADS_ACT_SILU>(z, v); break;
-    default: break;
-  }
-}
-
 // kN elements of D in a row, `step` apart along b: a, b + j step, of which the first `count` (at least one) exist.  `here`: row a exists (else
 // a is one that does, and nothing is stored).  Loads go to clamped places without a branch, so that they are all under way at
 // once, and come before the stores: out may be the residual.

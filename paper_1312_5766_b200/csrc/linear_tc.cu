@@ -432,8 +432,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       const Item w = item_of(g, first, split);
       const int row = threadIdx.x & (kRows - 1);
       const long long a = (long long)w.ta * kRows + row;
-      // a thread's columns: col, col + step, .., eight at a time
-      constexpr int kN = 8;
+      // a thread's columns: col, col + step, .., several at a time
+      constexpr int kN = S::kNarrow ? 4 : 8;
       const int step = 2 * g.splits, end = min(kBN, g.nb - w.tb * kBN);
       for (int col = split * 2 + (int)(threadIdx.x >> 7); col < end; col += kN * step) {
         const int count = min(kN, (end - col + step - 1) / step);
