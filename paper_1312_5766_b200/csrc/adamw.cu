@@ -30,7 +30,8 @@ namespace {
 
 constexpr int kBlock = 256;                    // elements that share a scale
 constexpr int kThreads = 256;
-constexpr long long kChunk = 2048;             // elements a CTA takes: a block for each of its warps
+constexpr int kTurns = 2;                       // blocks that a warp takes
+constexpr long long kChunk = (long long)kTurns * (kThreads / 32) * kBlock;      // elements that a CTA takes
 constexpr float kTiny = 7.888609052210118e-31f;      // 2^-100: a block whose largest magnitude is below is stored as noughts
 
 struct Entry {
@@ -75,62 +76,161 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return
 template <typename T> struct alignas(4 * sizeof(T)) Four { T x[4]; };
 
 // A lane's eight elements of a block of which n are there: two groups of four, at lane * 4 and 128 + lane * 4.
-// Elements that are not there read as 0.
-template <typename T, typename U>
-__device__ __forceinline__ void load8(const T* p, int n, bool vec, int lane, U (&x)[8]) {
+// kFull: all 256 are, and 16 bytes of them may be accessed at once.  Elements that are not there read as 0.
+template <typename T, bool kFull>
+__device__ __forceinline__ void load8(const T* p, int n, int lane, float (&x)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int i = h * 128 + lane * 4;
-    if (vec && i + 4 <= n) {
+    if (kFull) {
       const Four<T> f = *reinterpret_cast<const Four<T>*>(p + i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * h + j] = (U)f.x[j];
+      for (int j = 0; j < 4; ++j) x[4 * h + j] = (float)f.x[j];
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * h + j] = i + j < n ? (U)p[i + j] : (U)0.f;
+      for (int j = 0; j < 4; ++j) x[4 * h + j] = i + j < n ? (float)p[i + j] : 0.f;
     }
   }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, bool vec, int lane, const T (&x)[8]) {
+template <typename T, bool kFull>
+__device__ __forceinline__ void store8(T* p, int n, int lane, const float (&x)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int i = h * 128 + lane * 4;
-    if (vec && i + 4 <= n) {
+    if (kFull) {
       Four<T> f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f.x[j] = x[4 * h + j];
+      for (int j = 0; j < 4; ++j) f.x[j] = from_f32<T>(x[4 * h + j]);
       *reinterpret_cast<Four<T>*>(p + i) = f;
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) if (i + j < n) p[i + j] = x[4 * h + j];
+      for (int j = 0; j < 4; ++j) if (i + j < n) p[i + j] = from_f32<T>(x[4 * h + j]);
+    }
+  }
+}
+// The same for codes, four in a word.
+template <bool kFull>
+__device__ __forceinline__ void load_codes(const void* codes, int n, int lane, unsigned int (&w)[2]) {
+  const unsigned char* p = static_cast<const unsigned char*>(codes);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = h * 128 + lane * 4;
+    if (kFull) {
+      w[h] = *reinterpret_cast<const unsigned int*>(p + i);
+    } else {
+      w[h] = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (i + j < n) w[h] |= (unsigned int)p[i + j] << (8 * j);
+    }
+  }
+}
+template <bool kFull>
+__device__ __forceinline__ void store_codes(void* codes, int n, int lane, const unsigned int (&w)[2]) {
+  unsigned char* p = static_cast<unsigned char*>(codes);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = h * 128 + lane * 4;
+    if (kFull) {
+      *reinterpret_cast<unsigned int*>(p + i) = w[h];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (i + j < n) p[i + j] = (unsigned char)(w[h] >> (8 * j));
     }
   }
 }
 
-__device__ __forceinline__ bool finite(float mag) { return mag <= 3.402823466e38f; }      // (of a magnitude; false for NaN)
-__device__ __forceinline__ float warp_max(float mag) {                                      // magnitudes order like their bits
-  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mag)));
-}
 // Between codes and floats by the sum with 2^23 or 1.5 2^23, whose last bits then are the integer: the conversion instructions go through the
 // unit that the roots and quotients need, at a quarter of the rate.
 constexpr float kUnsigned = 8388608.f, kRounded = 12582912.f;
-__device__ __forceinline__ float decode_m(unsigned int byte, float s) {      // byte: the code as stored, -128 .. 127
-  const float q = __fsub_rn(__uint_as_float(0x4b000000u | (byte ^ 0x80u)), kUnsigned + 128.f);
-  return byte == 0x80u ? __uint_as_float(0x7fc00000u) : __fmul_rn(__fmul_rn(q, fabsf(q)), s);
+constexpr unsigned int kInfinity = 0x7f800000u;
+__device__ __forceinline__ unsigned int zero_bytes(unsigned int x) { return (x - 0x01010101u) & ~x & 0x80808080u; }      // not 0: there is one
+__device__ __forceinline__ float byte_as_float(unsigned int word, int j) {      // of byte j, plus kUnsigned
+  return __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7440u | (unsigned int)j));
 }
-__device__ __forceinline__ float decode_root(unsigned int byte, float s) {
-  const float q = __fsub_rn(__uint_as_float(0x4b000000u | byte), kUnsigned);
-  return byte == 255u ? __uint_as_float(0x7fc00000u) : __fmul_rn(__fmul_rn(q, q), s);
+// First moments, and roots of second ones, of eight codes.  The codes for what is not finite are looked for four at a time.
+__device__ __forceinline__ void decode_m(const unsigned int (&w)[2], float s, float (&m)[8]) {
+  const unsigned int x[2] = {w[0] ^ 0x80808080u, w[1] ^ 0x80808080u};      // the code plus 128: 0 stands for NaN
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float q = __fsub_rn(byte_as_float(x[j >> 2], j & 3), kUnsigned + 128.f);
+    m[j] = __fmul_rn(__fmul_rn(q, fabsf(q)), s);
+  }
+  if (zero_bytes(x[0]) | zero_bytes(x[1])) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (((x[j >> 2] >> (8 * (j & 3))) & 0xffu) == 0u) m[j] = __uint_as_float(0x7fc00000u);
+  }
 }
-// The integer nearest to the correctly rounded root of x (ties to even), x <= 2^16, in the last bits.  The approximate root is good to 2^-14
-// there; only where it lies within 2^-12 of the middle between two integers is the exact one needed.
-__device__ __forceinline__ unsigned int nearest_root(float x) {
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  float t = __fadd_rn(r, kRounded);
-  if (fabsf(fabsf(r - (t - kRounded)) - 0.5f) < 0.000244140625f) t = __fadd_rn(__fsqrt_rn(x), kRounded);
-  return __float_as_uint(t);
+__device__ __forceinline__ void decode_root(const unsigned int (&w)[2], float s, float (&root)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float q = __fsub_rn(byte_as_float(w[j >> 2], j & 3), kUnsigned);
+    root[j] = __fmul_rn(__fmul_rn(q, q), s);
+  }
+  if (zero_bytes(~w[0]) | zero_bytes(~w[1])) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (((w[j >> 2] >> (8 * (j & 3))) & 0xffu) == 255u) root[j] = __uint_as_float(0x7fc00000u);
+  }
+}
+// Magnitudes order like their bits; what is not finite comes last.  The largest finite one of the block's x (this lane's eight, and the other lanes').
+__device__ __forceinline__ float largest(const float (&x)[8], bool* all_finite) {
+  unsigned int top = 0u;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(fabsf(x[j])));
+  top = __reduce_max_sync(0xffffffffu, top);
+  *all_finite = top < kInfinity;
+  if (top >= kInfinity) {
+    top = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned int b = __float_as_uint(fabsf(x[j]));
+      if (b < kInfinity) top = max(top, b);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+  }
+  return __uint_as_float(top);
+}
+// Codes of eight values: the integer nearest to the correctly rounded root of |x| r (ties to even), with the value's sign.  The approximate root is
+// good to 2^-14 where it matters (up to 254); only where one lies within 2^-12 of the middle between two integers are the exact ones needed.
+// Without a sign, what is not 0 gets at least 1.
+template <bool kSigned>
+__device__ __forceinline__ void encode(const float (&x)[8], float r, bool all_finite, unsigned int (&w)[2]) {
+  float t[8];
+  bool near = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float root;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(__fmul_rn(fabsf(x[j]), r)));
+    if (kSigned) root = copysignf(root, x[j]);
+    t[j] = __fadd_rn(root, kRounded);
+    near = near || fabsf(__fsub_rn(root, __fsub_rn(t[j], kRounded))) > 0.499755859375f;
+  }
+  if (near) {
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+      float root = __fsqrt_rn(__fmul_rn(fabsf(x[j]), r));
+      if (kSigned) root = copysignf(root, x[j]);
+      const float v = __fadd_rn(root, kRounded);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (i == j) t[i] = v;
+    }
+  }
+  if (!kSigned)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = fmaxf(t[j], x[j] > 0.f ? kRounded + 1.f : kRounded);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    w[h] = __byte_perm(__byte_perm(__float_as_uint(t[4 * h]), __float_as_uint(t[4 * h + 1]), 0x0040u),
+                       __byte_perm(__float_as_uint(t[4 * h + 2]), __float_as_uint(t[4 * h + 3]), 0x0040u), 0x5410u);
+  if (!all_finite) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (__float_as_uint(fabsf(x[j])) >= kInfinity) {
+        const unsigned int at = 8u * (j & 3);
+        w[j >> 2] = (w[j >> 2] & ~(0xffu << at)) | ((kSigned ? 0x80u : 0xffu) << at);
+      }
+  }
 }
 
 // The scale of a block whose largest finite magnitude is `top`, and its inverse (both 0 where the block is stored as noughts).
@@ -151,6 +251,62 @@ __device__ __forceinline__ int find_tensor(const Table<kCap>& t) {
   return lo;
 }
 
+// One block of n elements from `at` on, by a warp.
+template <typename P, typename G, bool kMaster, int kBits, bool kFull>
+__device__ __forceinline__ void step_block(const Entry& e, const Scalars& c, long long at, int n, int lane) {
+  P* param = static_cast<P*>(e.param) + at;
+  float p[8], g[8], m[8], v[8];
+  if (kMaster) load8<float, kFull>(e.master + at, n, lane, p); else load8<P, kFull>(param, n, lane, p);
+  load8<G, kFull>(static_cast<const G*>(e.grad) + at, n, lane, g);
+  if (kBits == 32) {
+    load8<float, kFull>(static_cast<const float*>(e.m) + at, n, lane, m);
+    load8<float, kFull>(static_cast<const float*>(e.v) + at, n, lane, v);
+  } else {
+    unsigned int w1[2], w2[2];
+    load_codes<kFull>(static_cast<const unsigned char*>(e.m) + at, n, lane, w1);
+    load_codes<kFull>(static_cast<const unsigned char*>(e.v) + at, n, lane, w2);
+    const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
+    decode_m(w1, s1, m);
+    decode_root(w2, s2, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
+  }
+  float root[8], inv[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float gj = __fmul_rn(g[j], c.grad_scale);
+    m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(gj, c.ob1));
+    v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(gj, gj), c.ob2));
+    root[j] = __fsqrt_rn(v[j]);
+    inv[j] = __frcp_rn(__fadd_rn(__fmul_rn(root[j], c.unbias), c.eps));
+    p[j] = __fsub_rn(__fmul_rn(p[j], c.keep), __fmul_rn(__fmul_rn(m[j], c.move), inv[j]));
+  }
+  if (c.threshold > 0.f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float size = __fsub_rn(fabsf(p[j]), __fmul_rn(c.threshold, inv[j]));
+      p[j] = size < 0.f ? 0.f : copysignf(size, p[j]);      // (a NaN stays one)
+    }
+  }
+  store8<P, kFull>(param, n, lane, p);
+  if (kMaster) store8<float, kFull>(e.master + at, n, lane, p);
+  if (kBits == 32) {
+    store8<float, kFull>(static_cast<float*>(e.m) + at, n, lane, m);
+    store8<float, kFull>(static_cast<float*>(e.v) + at, n, lane, v);
+  } else {
+    unsigned int w[2];
+    float r;
+    bool all_finite;
+    const float s1 = scale_of(largest(m, &all_finite), 1.f / 16129.f, &r);
+    encode<true>(m, r, all_finite, w);
+    store_codes<kFull>(static_cast<unsigned char*>(e.m) + at, n, lane, w);
+    const float s2 = scale_of(largest(root, &all_finite), 1.f / 64516.f, &r);
+    encode<false>(root, r, all_finite, w);
+    store_codes<kFull>(static_cast<unsigned char*>(e.v) + at, n, lane, w);
+    if (lane == 0) { e.m_scale[at / kBlock] = s1; e.v_scale[at / kBlock] = s2; }
+  }
+}
+
 template <typename P, typename G, bool kMaster, int kBits, int kCap>
 __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Table<kCap> t, const __grid_constant__ Step s) {
   if (s.skip_dev != nullptr && *s.skip_dev != 0) return;
@@ -168,99 +324,44 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const __grid_constant__ Tabl
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int ti = find_tensor(t);
   const Entry& e = t.e[ti];
-  const bool vec = e.n_vec & 1;
-  const long long n_all = e.n_vec >> 1, at = (long long)((int)blockIdx.x - t.first[ti]) * kChunk + warp * kBlock;
-  if (at >= n_all) return;
-  const int n = (int)min((long long)kBlock, n_all - at);
-  P* param = static_cast<P*>(e.param) + at;
-  float p[8], g[8], m[8], v[8];
-  if (kMaster) load8(e.master + at, n, vec, lane, p); else load8(param, n, vec, lane, p);
-  load8(static_cast<const G*>(e.grad) + at, n, vec, lane, g);
-  if (kBits == 32) {
-    load8(static_cast<const float*>(e.m) + at, n, vec, lane, m);
-    load8(static_cast<const float*>(e.v) + at, n, vec, lane, v);
-  } else {
-    unsigned int q[8];
-    const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
-    load8(static_cast<const unsigned char*>(e.m) + at, n, vec, lane, q);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m[j] = decode_m(q[j], s1);
-    load8(static_cast<const unsigned char*>(e.v) + at, n, vec, lane, q);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float root = decode_root(q[j], s2);
-      v[j] = __fmul_rn(root, root);
-    }
+  const long long n_all = e.n_vec >> 1, first = (long long)((int)blockIdx.x - t.first[ti]) * kChunk + warp * kBlock;
+#pragma unroll 1
+  for (int i = 0; i < kTurns; ++i) {
+    const long long at = first + (long long)i * (kThreads / 32) * kBlock;
+    if (at >= n_all) return;
+    if ((e.n_vec & 1) && at + kBlock <= n_all) step_block<P, G, kMaster, kBits, true>(e, c, at, kBlock, lane);
+    else step_block<P, G, kMaster, kBits, false>(e, c, at, (int)min((long long)kBlock, n_all - at), lane);
   }
-  float root[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float gj = __fmul_rn(g[j], c.grad_scale);
-    m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(gj, c.ob1));
-    v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(gj, gj), c.ob2));
-    root[j] = __fsqrt_rn(v[j]);
-    const float inv = __frcp_rn(__fadd_rn(__fmul_rn(root[j], c.unbias), c.eps));
-    p[j] = __fsub_rn(__fmul_rn(p[j], c.keep), __fmul_rn(__fmul_rn(m[j], c.move), inv));
-    if (c.threshold > 0.f) {
-      const float size = __fsub_rn(fabsf(p[j]), __fmul_rn(c.threshold, inv));
-      p[j] = size < 0.f ? 0.f : copysignf(size, p[j]);      // (a NaN stays one)
-    }
-  }
-  P out[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) out[j] = from_f32<P>(p[j]);
-  store8(param, n, vec, lane, out);
-  if (kMaster) store8(e.master + at, n, vec, lane, p);
-  if (kBits == 32) {
-    store8(static_cast<float*>(e.m) + at, n, vec, lane, m);
-    store8(static_cast<float*>(e.v) + at, n, vec, lane, v);
-    return;
-  }
-  float top1 = 0.f, top2 = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float a = fabsf(m[j]);
-    if (finite(a)) top1 = fmaxf(top1, a);
-    if (finite(root[j])) top2 = fmaxf(top2, root[j]);
-  }
-  float r1, r2;
-  const float s1 = scale_of(warp_max(top1), 1.f / 16129.f, &r1), s2 = scale_of(warp_max(top2), 1.f / 64516.f, &r2);
-  unsigned char q1[8], q2[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float a = fabsf(m[j]);
-    const unsigned int q = nearest_root(__fmul_rn(a, r1)), w = nearest_root(__fmul_rn(root[j], r2));
-    q1[j] = (unsigned char)(finite(a) ? (m[j] < 0.f ? 0u - q : q) : 0x80u);
-    q2[j] = (unsigned char)(finite(root[j]) ? (root[j] > 0.f && (w & 0xffu) == 0u ? 1u : w) : 255u);
-  }
-  store8(static_cast<unsigned char*>(e.m) + at, n, vec, lane, q1);
-  store8(static_cast<unsigned char*>(e.v) + at, n, vec, lane, q2);
-  if (lane == 0) { e.m_scale[at / kBlock] = s1; e.v_scale[at / kBlock] = s2; }
 }
 
 // Moments held in 8 bits as the values that they stand for: entry.param receives m, entry.master v.
+template <bool kFull>
+__device__ __forceinline__ void unpack_block(const Entry& e, long long at, int n, int lane) {
+  const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
+  unsigned int w1[2], w2[2];
+  load_codes<kFull>(static_cast<const unsigned char*>(e.m) + at, n, lane, w1);
+  load_codes<kFull>(static_cast<const unsigned char*>(e.v) + at, n, lane, w2);
+  float m[8], v[8];
+  decode_m(w1, s1, m);
+  decode_root(w2, s2, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
+  store8<float, kFull>(static_cast<float*>(e.param) + at, n, lane, m);
+  store8<float, kFull>(e.master + at, n, lane, v);
+}
 template <int kCap>
 __global__ void __launch_bounds__(kThreads) k_adamw_unpack(const __grid_constant__ Table<kCap> t) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int ti = find_tensor(t);
   const Entry& e = t.e[ti];
-  const bool vec = e.n_vec & 1;
-  const long long n_all = e.n_vec >> 1, at = (long long)((int)blockIdx.x - t.first[ti]) * kChunk + warp * kBlock;
-  if (at >= n_all) return;
-  const int n = (int)min((long long)kBlock, n_all - at);
-  const float s1 = e.m_scale[at / kBlock], s2 = e.v_scale[at / kBlock];
-  unsigned int q1[8], q2[8];
-  load8(static_cast<const unsigned char*>(e.m) + at, n, vec, lane, q1);
-  load8(static_cast<const unsigned char*>(e.v) + at, n, vec, lane, q2);
-  float m[8], v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float root = decode_root(q2[j], s2);
-    m[j] = decode_m(q1[j], s1);
-    v[j] = __fmul_rn(root, root);
+  const long long n_all = e.n_vec >> 1, first = (long long)((int)blockIdx.x - t.first[ti]) * kChunk + warp * kBlock;
+#pragma unroll 1
+  for (int i = 0; i < kTurns; ++i) {
+    const long long at = first + (long long)i * (kThreads / 32) * kBlock;
+    if (at >= n_all) return;
+    if ((e.n_vec & 1) && at + kBlock <= n_all) unpack_block<true>(e, at, kBlock, lane);
+    else unpack_block<false>(e, at, (int)min((long long)kBlock, n_all - at), lane);
   }
-  store8(static_cast<float*>(e.param) + at, n, vec, lane, m);
-  store8(e.master + at, n, vec, lane, v);
 }
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
