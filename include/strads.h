@@ -351,12 +351,13 @@ typedef struct {
   strads_const_matrix_t x, w;
   float scale;
   uint32_t flags;
-  void* workspace;                      /* 256-byte aligned, as long as the call's query says (NULL if that is 0) */
+  void* workspace;                      /* 256-byte aligned; NULL, with workspace_bytes 0, for calls that need none */
   size_t workspace_bytes;
   void* stream;
 } strads_linear_config_t;
 
-/* Workspace of a forward pass, and of a backward pass whatever it is asked for (workspace fields of cfg are not read). */
+/* Workspace that is enough for a forward pass, and for a backward pass whatever it is asked for (workspace fields of cfg are not read).
+ * A call that needs less takes less: it is refused (STRADS_ERR_WORKSPACE_TOO_SMALL) only where it needs more than it is given. */
 int strads_linear_workspace_bytes(const strads_linear_config_t* cfg, size_t* forward_out, size_t* backward_out);
 int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, const strads_const_matrix_t* residual,
                           const strads_matrix_t* out, const strads_matrix_t* preact);

@@ -7,6 +7,7 @@ has not been built, importing its symbols raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -474,7 +475,7 @@ class AdamW:
     with 16-bit parameters, their float32 copies, which then take the step.  moments, where given, are used as they are and
     kept up to date: (first, second), lists of float32 tensors, with bits=32; (codes, scales, codes, scales), lists of
     int8, float32, uint8 and float32 tensors, with bits=8 (a scale per block of 256 elements).  Otherwise they are allocated
-    here, as noughts.
+    here, as noughts, in the parameters' shapes.
     """
 
     def __init__(self, params, bits=32, masters=None, moments=None, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, l1=0.0):
@@ -499,7 +500,7 @@ class AdamW:
         else:
             kinds = [(torch.int8, sizes), (torch.float32, blocks), (torch.uint8, sizes), (torch.float32, blocks)]
         if moments is None:
-            moments = [self._noughts(t, n, dev) for t, n in kinds]
+            moments = [self._noughts(t, [p.shape for p in params] if n is sizes else [(k,) for k in n], dev) for t, n in kinds]
         self.state = [list(m) for m in moments]
         if len(self.state) != len(kinds):
             raise ValueError(f"{len(kinds)} lists of moments expected with {bits} bits")
@@ -526,13 +527,13 @@ class AdamW:
                 e.m_scale, e.v_scale = self.state[1][i].data_ptr(), self.state[3][i].data_ptr()
 
     @staticmethod
-    def _noughts(dtype, sizes, dev):
+    def _noughts(dtype, shapes, dev):
         starts, total = [], 0
-        for n in sizes:                                  # every tensor's part starts on 16 bytes
+        for s in shapes:                                 # every tensor's part starts on 16 bytes
             starts.append(total)
-            total += -(-n // 16) * 16
+            total += -(-math.prod(s) // 16) * 16
         flat = torch.zeros(total, dtype=dtype, device=dev)
-        return [flat[a:a + n] for a, n in zip(starts, sizes)]
+        return [flat[a:a + math.prod(s)].view(s) for a, s in zip(starts, shapes)]
 
     def _check(self, what, tensors, dtype, sizes):
         if len(tensors) != len(sizes):
@@ -584,7 +585,7 @@ class AdamW:
             return self.state[0], self.state[1]
         sizes = [p.numel() for p in self.params]
         if out is None:
-            out = [self._noughts(torch.float32, sizes, self.device) for _ in range(2)]
+            out = [self._noughts(torch.float32, [p.shape for p in self.params], self.device) for _ in range(2)]
         first, second = (list(t) for t in out)
         self._check("values", first, torch.float32, sizes)
         self._check("values", second, torch.float32, sizes)

@@ -142,13 +142,14 @@ __global__ void __launch_bounds__(kThreads) k_linear_zero(T* p, long long rows, 
 }
 
 // ---- the order of kernels ----
-// A call is gone through twice by the same code: with s.run false to add up the workspace, then to launch.
+// A call is gone through twice by the same code: with `run` false to add up the workspace, then to launch.  `all`: a query for any call of
+// this configuration: everything is wanted, and where gout and the results will lie is not known.
 struct Call {
   int type;
   size_t size;                           // of an element
   char* ws;
   size_t used;
-  bool run, stall;
+  bool run, all, stall;
   cudaStream_t stream;
   cudaError_t err;
   unsigned int* status;
@@ -271,7 +272,7 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
   if (rows * 128 < g.n_rows) rows = (g.n_rows + 127) / 128;
   rows = (rows + 7) / 8 * 8;
   const int blocks = (int)((g.n_rows + rows - 1) / rows);
-  float* partial = gbias != nullptr || !c.run ? static_cast<float*>(c.take((size_t)blocks * (size_t)g.n_out * sizeof(float))) : nullptr;
+  float* partial = gbias != nullptr || c.all ? static_cast<float*>(c.take((size_t)blocks * (size_t)g.n_out * sizeof(float))) : nullptr;
   if (!c.run || c.err != cudaSuccess) return;
   const Operand o = operand_of(gout);
   Operand z = {};
@@ -308,20 +309,20 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
   const bool formed = g.activation != STRADS_ACT_IDENTITY;
   const long long ld = (g.n_out + 7) / 8 * 8;
   T* gz = formed ? static_cast<T*>(c.take((size_t)g.n_rows * (size_t)ld * sizeof(T))) : nullptr;
-  if (formed || gbias != nullptr || !c.run) gradient_of_z<T>(c, g, gout, preact, gz, ld, static_cast<T*>(gbias));
+  if (formed || gbias != nullptr || c.all) gradient_of_z<T>(c, g, gout, preact, gz, ld, static_cast<T*>(gbias));
   Operand kept = operand_of(gout);
   if (formed) { kept.p = gz; kept.rs = ld; kept.ks = 1; }
   Matrix z = matrix_of(kept, g.n_rows, g.n_out, 2), x = matrix_of(operand_of(g.x), g.n_rows, g.n_in, 0), w = matrix_of(operand_of(g.w), g.n_out, g.n_in, 1);
-  z.unknown = !formed && !c.run;
+  z.unknown = !formed && c.all;
   Finish f = {};
   f.plain = 1;
   f.scale = formed ? 1.f : g.scale;
-  if (gx != nullptr || !c.run) {
+  if (gx != nullptr || c.all) {
     const bool ar = gx != nullptr && rows_run(gx->row_stride, gx->col_stride);
     if (gx != nullptr) f.out = side(gx->data, gx->row_stride, gx->col_stride, ar);
     if (ar) product(c, z, false, w, true, f); else product(c, w, true, z, false, f);
   }
-  if (gw != nullptr || !c.run) {
+  if (gw != nullptr || c.all) {
     const bool ar = gw != nullptr && rows_run(gw->row_stride, gw->col_stride);
     if (gw != nullptr) f.out = side(gw->data, gw->row_stride, gw->col_stride, ar);
     if (ar) product(c, z, true, x, true, f); else product(c, x, true, z, true, f);
@@ -333,10 +334,10 @@ void backward_of(Call& c, const strads_linear_config_t& g, const strads_const_ma
   else if (g.type == STRADS_BF16) backward<__nv_bfloat16>(c, g, gout, preact, gx, gw, gbias);
   else backward<__half>(c, g, gout, preact, gx, gw, gbias);
 }
-Call call_of(const strads_linear_config_t& g, bool run) {
+Call call_of(const strads_linear_config_t& g, bool run, bool all) {
   Call c = {};
   c.type = g.type; c.size = g.type == STRADS_F32 ? 4 : 2;
-  c.run = run; c.stall = (g.flags & STRADS_LINEAR_FLAG_STALL) != 0;
+  c.run = run; c.all = all; c.stall = (g.flags & STRADS_LINEAR_FLAG_STALL) != 0;
   c.ws = run ? static_cast<char*>(g.workspace) : nullptr;
   c.stream = static_cast<cudaStream_t>(g.stream);
   c.err = cudaSuccess;
@@ -383,7 +384,7 @@ int strads_linear_workspace_bytes(const strads_linear_config_t* cfg, size_t* for
   if (cfg == nullptr || forward_out == nullptr || backward_out == nullptr) return STRADS_ERR_INVALID_ARG;
   const int rc = check(*cfg);
   if (rc != STRADS_OK) return rc;
-  Call f = call_of(*cfg, false), b = call_of(*cfg, false);
+  Call f = call_of(*cfg, false, true), b = call_of(*cfg, false, true);
   if (cfg->n_rows > 0) {
     forward(f, *cfg, nullptr, nullptr, nullptr, nullptr);
     backward_of(b, *cfg, strads_const_matrix_t{nullptr, 0, 0}, nullptr, nullptr, nullptr, nullptr);
@@ -393,19 +394,15 @@ int strads_linear_workspace_bytes(const strads_linear_config_t* cfg, size_t* for
   return STRADS_OK;
 }
 
-static int check_workspace(const strads_linear_config_t& c, int which) {
-  size_t need[2];
-  const int rc = strads_linear_workspace_bytes(&c, &need[0], &need[1]);
-  if (rc != STRADS_OK) return rc;
-  if (need[which] == 0) return STRADS_OK;
-  if (c.workspace_bytes < need[which]) return STRADS_ERR_WORKSPACE_TOO_SMALL;
-  return c.workspace == nullptr || ((uintptr_t)c.workspace & 255) != 0 ? STRADS_ERR_INVALID_ARG : STRADS_OK;
+static int check_workspace(const strads_linear_config_t& c, size_t need) {
+  if (c.workspace_bytes < need) return STRADS_ERR_WORKSPACE_TOO_SMALL;
+  return need > 0 && (c.workspace == nullptr || ((uintptr_t)c.workspace & 255) != 0) ? STRADS_ERR_INVALID_ARG : STRADS_OK;
 }
 
 int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, const strads_const_matrix_t* residual,
                           const strads_matrix_t* out, const strads_matrix_t* preact) {
   if (cfg == nullptr) return STRADS_ERR_INVALID_ARG;
-  int rc = check_workspace(*cfg, 0);
+  int rc = check(*cfg);
   if (rc != STRADS_OK) return rc;
   const strads_linear_config_t& c = *cfg;
   if (c.n_rows == 0) return STRADS_OK;
@@ -413,7 +410,10 @@ int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, c
   if (out == nullptr || !valid_out(*out, size, c.n_rows, c.n_out) || (preact != nullptr && !valid_out(*preact, size, c.n_rows, c.n_out)) ||
       (residual != nullptr && !valid_in(*residual, size)) || ((uintptr_t)bias % size) != 0)
     return STRADS_ERR_INVALID_ARG;
-  Call call = call_of(c, true);
+  Call sizes = call_of(c, false, false);
+  forward(sizes, c, bias, residual, out, preact);
+  if ((rc = check_workspace(c, sizes.used)) != STRADS_OK) return rc;
+  Call call = call_of(c, true, false);
   forward(call, c, bias, residual, out, preact);
   return call.err == cudaSuccess ? STRADS_OK : cuda_failed(call.err, "strads_linear_forward");
 }
@@ -421,7 +421,7 @@ int strads_linear_forward(const strads_linear_config_t* cfg, const void* bias, c
 int strads_linear_backward(const strads_linear_config_t* cfg, const strads_const_matrix_t* gout, const strads_const_matrix_t* preact,
                            const strads_matrix_t* gx, const strads_matrix_t* gw, void* gbias) {
   if (cfg == nullptr) return STRADS_ERR_INVALID_ARG;
-  int rc = check_workspace(*cfg, 1);
+  int rc = check(*cfg);
   if (rc != STRADS_OK) return rc;
   const strads_linear_config_t& c = *cfg;
   const int size = c.type == STRADS_F32 ? 4 : 2;
@@ -434,7 +434,10 @@ int strads_linear_backward(const strads_linear_config_t* cfg, const strads_const
   if (gx == nullptr && gw == nullptr && gbias == nullptr) return STRADS_OK;
   const strads_const_matrix_t none = {nullptr, 0, 0};
   const strads_const_matrix_t& g = gout ? *gout : none;
-  Call call = call_of(c, true);
+  Call sizes = call_of(c, false, false);
+  backward_of(sizes, c, g, preact, gx, gw, gbias);
+  if ((rc = check_workspace(c, sizes.used)) != STRADS_OK) return rc;
+  Call call = call_of(c, true, false);
   backward_of(call, c, g, preact, gx, gw, gbias);
   return call.err == cudaSuccess ? STRADS_OK : cuda_failed(call.err, "strads_linear_backward");
 }

@@ -279,6 +279,21 @@ def test_scalars_on_the_device_in_a_captured_step(b, bits):
             assert torch.equal(x, y), t
 
 
+def test_a_solution_of_the_lasso_is_where_the_step_rests(b):
+    """Eq. 1's optimality conditions: the gradient is -lambda sign(beta_j) where beta_j is not 0, within lambda elsewhere.  With the moments
+    at rest there (m = g, v = g^2) a step moves beta_j by lr lambda / d and its threshold takes that back: what is left are the roundings
+    of the three terms, at most 16 of half a step each."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    n, lam = 5000, 0.3
+    beta = torch.randn(n, generator=gen, device="cuda") * (torch.rand(n, generator=gen, device="cuda") < 0.3)
+    g = torch.where(beta != 0, -lam * beta.sign(), lam * 0.99 * (2 * torch.rand(n, generator=gen, device="cuda") - 1))
+    p = beta.clone()
+    opt = b.AdamW([p], moments=([g.clone()], [g * g]), l1=lam, betas=(B1, B2), eps=EPS)
+    opt.step([g], lr=LR, step=10_000_000)                # (so far on that no moment is corrected)
+    assert ((p == 0) == (beta == 0)).all()
+    assert ((p - beta).abs() <= 16 * 2.0 ** -24 * (beta.abs() + 2 * LR)).all()
+
+
 def test_on_another_stream(b):
     s = torch.cuda.Stream()
     p, g = torch.randn(1_000_000, device="cuda"), torch.randn(1_000_000, device="cuda")

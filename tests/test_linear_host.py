@@ -79,10 +79,14 @@ def test_workspace(b):
     assert lib.strads_linear_workspace_bytes(C.byref(_config(b)), None, None) == -1
     c = _config(b, type=0, n_rows=1000, n_in=1000, n_out=1000)
     assert query(C.byref(c)) == 0 and need[1] > 0
-    c.workspace_bytes = need[1] - 1
-    assert _call(b, c, "backward") == -3
+    assert need[0] >= 6 * 2 * 1000 * 1000                # two operands as three bfloat16 planes
+    c.x_row_stride = c.w_row_stride = 1000
+    full = dict(gx=b.Matrix(0x500000, 1000, 1), gw=b.Matrix(0x600000, 1000, 1), gout=b.Matrix(0x300000, 1000, 1), preact=b.Matrix(0x400000, 1000, 1))
+    c.workspace_bytes = 256
+    assert _call(b, c, "backward", **full) == -3
+    assert _call(b, c, "forward", out=b.Matrix(0x300000, 1000, 1)) == -3
     c.workspace, c.workspace_bytes = None, need[1]
-    assert _call(b, c, "backward") == -1
+    assert _call(b, c, "backward", **full) == -1
     # no rows: nothing to do, whatever the pointers
     c = _config(b, n_rows=0)
     c.x = None
