@@ -91,7 +91,7 @@ __device__ __forceinline__ void stage_short(const Thin& t, long long k0, int n, 
 // kDirect: the short side is read as it is (16-byte accesses to both sides).
 template <typename T, int kT, int kR, bool kDirect>
 __global__ void __launch_bounds__(kThreads) k_thin_k(const __grid_constant__ Thin t) {
-  constexpr int kV = 16 / sizeof(T), kStage = kStageFloats / kT, kU = kR * kT <= 2 ? 8 : 4;
+  constexpr int kV = 16 / sizeof(T), kStage = kStageFloats / kT, kU = sizeof(T) == 2 && kR * kT <= 2 ? 8 : 4;
   __shared__ __align__(16) float sh[kDirect ? 4 : kStageFloats];
   __shared__ float red[kWarps][kR * kT];
   __shared__ float sum[kWarps][kR * kT];
