@@ -30,8 +30,10 @@ struct Sizes {
   static constexpr int kStageBytes = kLongBytes + kShortBytes;
   static constexpr int kStages = (227 * 1024 - 2048) / kStageBytes;
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024;
-  static constexpr uint32_t kD = 3 * kBN, kA = 2 * kD;      // tensor memory: two sets of accumulators, then two of the long side's planes (96 columns each)
-  static_assert(kA + 2 * 96 <= 512 && kShortBytes % 1024 == 0, "");
+  // tensor memory: two sets of accumulators, then as many of the long side's planes (96 columns each) as fit: with two, splitting waited for the products
+  static constexpr uint32_t kD = 3 * kBN, kA = 2 * kD;
+  static constexpr int kSets = (512 - (int)kA) / 96;
+  static_assert(kSets >= 2 && kShortBytes % 1024 == 0, "");
 };
 
 struct SplitArgs {
@@ -92,21 +94,22 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   using Z = Sizes<kBN>;
   constexpr int kStages = Z::kStages;
   extern __shared__ unsigned char dyn[];
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_afull[2], s_aempty[2], s_tfull[2], s_tempty[2];
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[kStages], s_sempty[kStages], s_afull[Z::kSets], s_aempty[Z::kSets], s_tfull[2], s_tempty[2];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u;
-  const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), afull = smem_u32(s_afull), aempty = smem_u32(s_aempty), tfull = smem_u32(s_tfull),
+  const uint32_t ring = (smem_u32(dyn) + 1023u) & ~1023u, shorts = ring + kStages * kLongBytes;
+  const uint32_t full = smem_u32(s_full), empty = smem_u32(s_empty), sfull = smem_u32(s_sfull), sempty = smem_u32(s_sempty), afull = smem_u32(s_afull), aempty = smem_u32(s_aempty), tfull = smem_u32(s_tfull),
                  tempty = smem_u32(s_tempty);
   const uint32_t limit = g.stall ? kMmaStallLimit : kMmaWaitLimit;
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int i = 0; i < kStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(afull + 8 * i, kSplitWarps / 2); mbar_init(aempty + 8 * i, 1);
-      mbar_init(tfull + 8 * i, 1); mbar_init(tempty + 8 * i, kEpiWarps);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kSplitWarps / 2);
+      mbar_init(sfull + 8 * i, 1); mbar_init(sempty + 8 * i, 1);
     }
+    for (int i = 0; i < Z::kSets; ++i) { mbar_init(afull + 8 * i, kSplitWarps / 2); mbar_init(aempty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(tfull + 8 * i, 1); mbar_init(tempty + 8 * i, kEpiWarps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_l) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_s) : "memory");
@@ -125,33 +128,39 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   Walk at(g, u0);
 
   if (warp == kTmaWarp) {
-    if (lane == 0) {
+    if (elect_one()) {
       bool ok = true;
       int n = 0;
       for (; n < run; ++n, at.next(g)) {
-        const uint32_t s = (uint32_t)(n % kStages), to = ring + s * Z::kStageBytes;
-        ok = !s_abort && mbar_wait(empty + 8 * s, ((uint32_t)(n / kStages) & 1u) ^ 1u, limit) && !g.stall;
+        // the long side's ring is free again when a block has been split, the short side's when the products have read it
+        const uint32_t s = (uint32_t)(n % kStages), parity = ((uint32_t)(n / kStages) & 1u) ^ 1u, to = ring + s * kLongBytes;
+        ok = !s_abort && mbar_wait(empty + 8 * s, parity, limit) && !g.stall;
         if (!ok) break;
         int tl, ts;
         tile_of(g, at.tile, &tl, &ts);
         const int k0 = at.block * kBlockK, l0 = tl * kRows;
-        mbar_expect(full + 8 * s, (uint32_t)Z::kStageBytes);
+        mbar_expect(full + 8 * s, (uint32_t)kLongBytes);
         if (g.l_rows_inner) {
           tma_load_raw(to, &map_l, l0, k0, full + 8 * s);
         } else {
           tma_load_raw(to, &map_l, k0, l0, full + 8 * s);
           tma_load_raw(to + kLongBytes / 2, &map_l, k0 + 32, l0, full + 8 * s);
         }
+        ok = mbar_wait(sempty + 8 * s, parity, limit);
+        if (!ok) { ++n; break; }                         // (the long side's load is under way all the same)
+        mbar_expect(sfull + 8 * s, (uint32_t)Z::kShortBytes);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) tma_load<1>(to + kLongBytes + p * kBN * 128, &map_s, k0, ts * kBN, p, full + 8 * s);
+        for (int p = 0; p < 3; ++p) tma_load<1>(shorts + s * Z::kShortBytes + p * kBN * 128, &map_s, k0, ts * kBN, p, sfull + 8 * s);
       }
       if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
       // every stage filled is used up before the shared memory goes; having given up, what is under way gets its time to land
-      for (int j = n > kStages ? n - kStages : 0; j < n; ++j)
-        if (!mbar_wait((ok ? empty : full) + 8 * (uint32_t)(j % kStages), (uint32_t)(j / kStages) & 1u, limit)) {
+      for (int j = n > kStages ? n - kStages : 0; j < n; ++j) {
+        const uint32_t at8 = 8 * (uint32_t)(j % kStages), parity = (uint32_t)(j / kStages) & 1u;
+        if (!mbar_wait((ok ? empty : full) + at8, parity, limit) || !mbar_wait((ok ? sempty : sfull) + at8, parity, limit)) {
           if (ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
           break;
         }
+      }
     }
     __syncwarp();
   } else if (warp >= kEpiWarps && warp < kEpiWarps + kSplitWarps) {
@@ -159,12 +168,13 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
     const int row = (warp & 3) * 32 + lane, group = (warp - kEpiWarps) >> 2;
     bool ok = true;
     for (int n = group; n < run; n += 2) {
-      const uint32_t s = (uint32_t)(n % kStages), from = ring + s * Z::kStageBytes;
+      const uint32_t s = (uint32_t)(n % kStages), from = ring + s * kLongBytes;
+      const uint32_t b = (uint32_t)(n % Z::kSets);
       ok = !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kStages) & 1u, limit) &&
-           mbar_wait(aempty + 8 * group, (((uint32_t)n >> 1) & 1u) ^ 1u, limit);
+           mbar_wait(aempty + 8 * b, ((uint32_t)(n / Z::kSets) & 1u) ^ 1u, limit);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t to = tmem + Z::kA + group * 96 + ((uint32_t)((warp & 3) * 32) << 16);
+      const uint32_t to = tmem + Z::kA + b * 96 + ((uint32_t)((warp & 3) * 32) << 16);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         uint32_t p0[16], p1[16], p2[16];
@@ -197,44 +207,52 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
         tmem_store16(to + half * 16 + 32, p1);
         tmem_store16(to + half * 16 + 64, p2);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty + 8 * s);         // (all of it has been read into registers)
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(afull + 8 * group);
+      if (lane == 0) mbar_arrive(afull + 8 * b);
     }
     if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     __syncwarp();
-  } else if (warp == kMmaWarp) {
-    if (lane == 0) {
+  } else if (warp == kMmaWarp) {                         // (the warp as one; an elected lane issues)
+    {
+      const bool one = elect_one();
       constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24);      // bfloat16, k along memory in B
       bool ok = true;
       uint32_t v = 0;
       for (int n = 0; n < run && ok; ++v) {
         // a segment: up to kSegment blocks of one tile
         const int len = min(min(kSegment, run - n), g.blocks - at.block);
-        ok = !s_abort && mbar_wait(tempty + 8 * (v & 1u), ((v >> 1) & 1u) ^ 1u, limit);
+        ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(tempty + 8 * (v & 1u), ((v >> 1) & 1u) ^ 1u, limit));
         if (!ok) break;
         const uint32_t d = tmem + (v & 1u) * Z::kD;
         for (int i = 0; i < len; ++i, ++n, at.next(g)) {
-          const uint32_t s = (uint32_t)(n % kStages), b = n & 1;
-          ok = !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kStages) & 1u, limit) && mbar_wait(afull + 8 * b, ((uint32_t)n >> 1) & 1u, limit);
+          const uint32_t s = (uint32_t)(n % kStages), b = (uint32_t)(n % Z::kSets);
+          ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(sfull + 8 * s, (uint32_t)(n / kStages) & 1u, limit) &&
+                                       mbar_wait(afull + 8 * b, (uint32_t)(n / Z::kSets) & 1u, limit));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint64_t db = umma_desc(ring + s * Z::kStageBytes + kLongBytes, false);
+          const uint64_t db = umma_desc(shorts + s * Z::kShortBytes, false);
           const uint32_t da = tmem + Z::kA + b * 96;
+          if (one) {
 #pragma unroll
-          for (int j = 0; j < kBlockK / 16; ++j) {
-            umma_a_tmem(d, da + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(3 * kBN >> 3) << 17), i > 0 || j > 0);
-            umma_a_tmem(d + kBN, da + 32 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(2 * kBN >> 3) << 17), 1);
-            umma_a_tmem(d + 2 * kBN, da + 64 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(kBN >> 3) << 17), 1);
+            for (int j = 0; j < kBlockK / 16; ++j) {
+              umma_a_tmem(d, da + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(3 * kBN >> 3) << 17), i > 0 || j > 0);
+              umma_a_tmem(d + kBN, da + 32 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(2 * kBN >> 3) << 17), 1);
+              umma_a_tmem(d + 2 * kBN, da + 64 + j * 8, db + (uint64_t)(j * 2), kDesc | ((uint32_t)(kBN >> 3) << 17), 1);
+            }
+            umma_commit<1>(sempty + 8 * s);
+            umma_commit<1>(aempty + 8 * b);
           }
-          umma_commit<1>(empty + 8 * s);
-          umma_commit<1>(aempty + 8 * b);
+          __syncwarp();
         }
         if (!ok) break;
-        umma_commit<1>(tfull + 8 * (v & 1u));
+        if (one) umma_commit<1>(tfull + 8 * (v & 1u));
+        __syncwarp();
       }
-      if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
+      if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     }
     __syncwarp();
   } else {

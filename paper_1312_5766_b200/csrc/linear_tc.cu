@@ -234,7 +234,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   const int n_items = g.tiles_a * g.tiles_b;
 
   if (warp == kTmaWarp) {
-    if (lane == 0) {
+    if (elect_one()) {
       uint32_t n = 0;                                    // stages filled so far
       bool ok = true;
       const uint32_t bytes = (uint32_t)(S::kABytes + (g.b_rows_inner ? (S::kCols < 64 ? 64 : S::kCols) : S::kCols) * 128);
@@ -287,7 +287,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
-    if (lane == 0 && leader) {
+    if (leader) {                                        // (the warp as one; an elected lane issues)
+      const bool one = elect_one();
       const uint32_t idesc = (1u << 4) | ((uint32_t)g.bf16 << 7) | ((uint32_t)g.bf16 << 10) | ((uint32_t)g.a_rows_inner << 15) |
                              ((uint32_t)g.b_rows_inner << 16) | ((uint32_t)(kBN >> 3) << 17) | ((uint32_t)(kRows * kCG >> 4) << 24);
       const uint32_t adv_a = g.a_rows_inner ? 128 : 2, adv_b = g.b_rows_inner ? 128 : 2;      // 16 k on, in units of 16 bytes
@@ -298,27 +299,31 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const int seg = kPlanes ? kSegment : w.blocks;
         for (int k = 0; k < w.blocks && ok; k += seg, ++u) {
           const int steps = min(seg, w.blocks - k) * (kPlanes ? kProducts : 1);
-          ok = !s_abort && mbar_wait(tempty + 8 * (u & 1u), ((u >> 1) & 1u) ^ 1u, limit);
+          ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(tempty + 8 * (u & 1u), ((u >> 1) & 1u) ^ 1u, limit));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t d = tmem + (u & 1u) * kBN;
           for (int it = 0; it < steps; ++it, ++n) {
             const uint32_t s = n % S::kStages;
-            ok = !s_abort && mbar_wait(full + 8 * s, (n / S::kStages) & 1u, limit);
+            ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(full + 8 * s, (n / S::kStages) & 1u, limit));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t sa = tiles + s * S::kStageBytes;
             const uint64_t da = umma_desc(sa, g.a_rows_inner), db = umma_desc(sa + S::kABytes, g.b_rows_inner);
+            if (one) {
 #pragma unroll
-            for (int j = 0; j < kBlockK / 16; ++j)
-              umma<kCG>(d, da + (uint64_t)(j * adv_a), db + (uint64_t)(j * adv_b), idesc, it > 0 || j > 0);
-            umma_commit<kCG>(empty + 8 * s);
+              for (int j = 0; j < kBlockK / 16; ++j)
+                umma<kCG>(d, da + (uint64_t)(j * adv_a), db + (uint64_t)(j * adv_b), idesc, it > 0 || j > 0);
+              umma_commit<kCG>(empty + 8 * s);
+            }
+            __syncwarp();
           }
           if (!ok) break;
-          umma_commit<kCG>(tfull + 8 * (u & 1u));
+          if (one) umma_commit<kCG>(tfull + 8 * (u & 1u));
+          __syncwarp();
         }
       }
-      if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
+      if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     }
     __syncwarp();
   } else {
