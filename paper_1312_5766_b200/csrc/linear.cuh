@@ -28,9 +28,9 @@ __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_f32(__half* p, float v) { *p = __float2half_rn(v); }
 
-// Functions for binary32 results (kExact) by CUDA's own, for 16-bit ones to 2^-20: the hardware's exponential and quotient, and
-// Phi(-z), z >= 0, as exp(-z^2/2) t P(t), t = 1 / (1 + 0.285 z): P is fitted to erfcx, weighted so that the relative error is even
-// (1.6e-7; 4.7e-7 as evaluated here).  Nothing cancels for negative z in any of them.
+// For binary32 results (kExact) CUDA's exponential and quotient, for 16-bit ones the hardware's, good to 2^-20.  Phi(-z), z >= 0, is exp(-z^2/2)
+// t P(t), t = 1 / (1 + 0.285 z): P is fitted to erfcx, weighted so that the relative error is even (1.6e-7; 4.7e-7 as evaluated here).  Nothing
+// cancels for negative z in any of them.
 template <bool kExact>
 __device__ __forceinline__ float sigmoid_f32(float z) { return kExact ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z)); }
 __device__ __forceinline__ float normal_tail(float a, float e) {      // Phi(-a), e = exp(-a^2/2)
@@ -54,8 +54,7 @@ __device__ __forceinline__ float activate_as(float z) {
   if (kAct == STRADS_ACT_RELU) return z < 0.f ? 0.f : z;               // (a NaN stays one)
   if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z);
   if (kAct == STRADS_ACT_GELU) {
-    if (kExact) return z * normcdff(z);
-    const float q = z * normal_tail(fabsf(z), __expf(-0.5f * z * z));
+    const float q = z * normal_tail(fabsf(z), kExact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
     return z > 0.f ? z - q : q;
   }
   if (kAct == STRADS_ACT_GELU_TANH) return z * sigmoid_f32<kExact>(tanh_argument2(z));
@@ -69,14 +68,8 @@ __device__ __forceinline__ float slope_as(float z) {
   if (kAct == STRADS_ACT_GELU) {
     const float e = kExact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
     const float near = fminf(fmaxf(z, -40.f), 40.f);                   // (beyond, e is 0)
-    float phi;
-    if (kExact) {
-      phi = normcdff(z);
-    } else {
-      const float q = normal_tail(fabsf(z), e);
-      phi = z > 0.f ? 1.f - q : q;
-    }
-    return fmaf(near * 0.3989422804014327f, e, phi);
+    const float q = normal_tail(fabsf(z), e);
+    return fmaf(near * 0.3989422804014327f, e, z > 0.f ? 1.f - q : q);
   }
   if (kAct == STRADS_ACT_GELU_TANH) {
     const float u = tanh_argument2(z), near = fminf(fmaxf(z, -40.f), 40.f);      // (beyond, the second term is 0)

@@ -7,9 +7,9 @@
 // kCG = 2: two CTAs of a cluster share a tile of 256 rows, each holding its 128 rows of A and half of B, which halves what is
 // loaded per product; the first one issues the MMAs for both.
 //
-// binary32 operands come as three bfloat16 planes, x = p0 + p1 + p2 (24 bits).  Of the nine products of planes the six largest are formed,
-// the smallest first.  The accumulator is emptied into registers every kSegment blocks of k and added there with rounding to nearest: the
-// tensor cores' additions truncate, which over a long k would cost more than the parts left out.
+// binary32 operands come as three bfloat16 planes, x = p0 + p1 + p2 (24 bits).  A stage holds all of them for its 64 k, and of the nine products
+// of planes the six largest are formed, the smallest first.  The accumulator is emptied into registers after every block of k and added there with
+// rounding to nearest: the tensor cores' additions truncate (100,000 terms of one sign summed there: 2e-5 too small).
 //
 // Few tiles: the CTAs of a cluster share a tile's k (splits > 1, kCG = 1), park their sums in shared memory and each finishes a share
 // of the columns, adding in the order of the CTAs.
@@ -31,24 +31,25 @@ constexpr int kBlockK = 64;                // 16-bit elements of k per stage = o
 constexpr int kEpiWarps = 8;
 constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
 constexpr int kThreads = 32 * (kEpiWarps + 2);
-constexpr int kSegment = 4;                // blocks of k between two emptyings of the accumulator (binary32)
-constexpr int kProducts = 6;
+constexpr int kProducts = 6;               // of planes (binary32)
 constexpr uint32_t kWaitLimit = kMmaWaitLimit, kStallLimit = kMmaStallLimit;
 constexpr size_t kSmemMost = 227 * 1024;
 
-template <int kBN, int kCG>
+template <typename T, int kBN, int kCG>
 struct Shape {
+  static constexpr bool kPlanes = sizeof(T) == 4;
   static constexpr int kCols = kBN / kCG;                                  // rows of B that a CTA holds
   static constexpr int kABytes = kRows * 128;
   static constexpr int kBBytes = (kCols < 64 ? 64 : kCols) * 128;          // (a box along the rows is at least 64 wide)
-  static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kChunk = kBN < 128 ? 16 : 32;              // columns of a 16-bit result that a warp finishes at a time (binary32: 16)
+  static constexpr int kStageBytes = (kPlanes ? 3 : 1) * (kABytes + kBBytes);
+  static constexpr int kChunk = kPlanes || kBN < 128 ? 16 : 32;           // columns of the result that a warp finishes at a time
   static constexpr int kSlotBytes = 2048;                                 // a chunk: 32 rows of them
   // narrow tiles read far more than they write: no shared memory for results, and two CTAs to an SM, so that up to 2 x 148 tiles
   // are under way at once and share the memory's bandwidth evenly however they divide by 148
   static constexpr bool kNarrow = kBN < 128;
-  static constexpr int kEpiBytes = kNarrow ? 0 : kEpiWarps * 4 * kSlotBytes;      // per warp two slots for what comes in and two for what goes out
-  static constexpr int kStages = (int)(((kNarrow ? kSmemMost / 2 - 512 : kSmemMost) - 2048 - kEpiBytes) / kStageBytes);
+  // per warp two slots for what goes out and two for what comes in (binary32: the residual comes straight, 128 bytes an instruction)
+  static constexpr int kEpiBytes = kNarrow ? 0 : kEpiWarps * (kPlanes ? 2 : 4) * kSlotBytes;
+  static constexpr int kStages = (int)(((kNarrow && !kPlanes ? kSmemMost / 2 - 512 : kSmemMost) - 2048 - kEpiBytes) / kStageBytes);
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpiBytes + 1024;
   static constexpr uint32_t kTmemCols = 2 * kBN < 32 ? 32 : 2 * kBN;      // two accumulators
   static_assert(kBN * kRows * 4 <= kStages * kStageBytes, "the parked sums take the ring's place");
@@ -63,15 +64,6 @@ __device__ __forceinline__ Item item_of(const TcArgs& g, int i, int split) {
   const int per = kGroup * g.tiles_b, first = i / per * kGroup, high = min(kGroup, g.tiles_a - first), in = i % per;
   return {first + in % high, in / high, (g.blocks - split + g.splits - 1) / g.splits};
 }
-// Block (of this CTA's) and planes that come `it`-th in a segment of `len` blocks from k0 on.  Smallest products first.
-struct Step { int kb, pa, pb; };
-template <bool kPlanes>
-__device__ __forceinline__ Step step_of(int k0, int len, int it) {
-  if (!kPlanes) return {k0 + it, 0, 0};
-  const int q = it / len;
-  return {k0 + it % len, (0x201100 >> (4 * (5 - q))) & 3, (0x021010 >> (4 * (5 - q))) & 3};
-}
-
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
@@ -184,11 +176,11 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
 }
 
 template <typename T, int kBN, int kCG>
-__global__ void __launch_bounds__(kThreads, kBN < 128 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, kBN < 128 && sizeof(T) == 2 ? 2 : 1)
 k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
             const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ TcArgs g) {
-  using S = Shape<kBN, kCG>;
-  constexpr bool kPlanes = sizeof(T) == 4;
+  using S = Shape<T, kBN, kCG>;
+  constexpr bool kPlanes = S::kPlanes;
   constexpr int kHalf = kBN / 2;                         // columns of a tile that an epilogue warp reads back
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_tfull[2], s_tempty[2], s_in[kEpiWarps][2];
@@ -237,35 +229,32 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     if (elect_one()) {
       uint32_t n = 0;                                    // stages filled so far
       bool ok = true;
-      const uint32_t bytes = (uint32_t)(S::kABytes + (g.b_rows_inner ? (S::kCols < 64 ? 64 : S::kCols) : S::kCols) * 128);
+      const uint32_t bytes = (kPlanes ? 3u : 1u) * (uint32_t)(S::kABytes + (g.b_rows_inner ? (S::kCols < 64 ? 64 : S::kCols) : S::kCols) * 128);
       for (int i = first; i < n_items && ok; i += stride) {
         const Item w = item_of(g, i, split);
         const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0), b0 = w.tb * kBN + (kCG == 2 ? (int)rank * S::kCols : 0);
-        const int seg = kPlanes ? kSegment : w.blocks;
-        for (int k = 0; k < w.blocks && ok; k += seg) {
-          const int len = min(seg, w.blocks - k), steps = len * (kPlanes ? kProducts : 1);
-          for (int it = 0; it < steps; ++it, ++n) {
-            const uint32_t s = n % S::kStages;
-            ok = !s_abort && mbar_wait(empty + 8 * s, ((n / S::kStages) & 1u) ^ 1u, limit);
-            if (!ok) break;
-            if (g.stall) continue;                       // (withheld: the consumers' waits run out)
-            Step st = step_of<kPlanes>(k, len, it);
-            st.kb = st.kb * g.splits + split;
-            const uint32_t bar = kCG == 2 ? mapa(full + 8 * s, 0) : full + 8 * s;
-            if (leader) mbar_expect(full + 8 * s, bytes * kCG);
-            const uint32_t sa = tiles + s * S::kStageBytes, sb = sa + S::kABytes;
+        for (int k = 0; k < w.blocks; ++k, ++n) {
+          const uint32_t s = n % S::kStages;
+          ok = !s_abort && mbar_wait(empty + 8 * s, ((n / S::kStages) & 1u) ^ 1u, limit);
+          if (!ok) break;
+          if (g.stall) continue;                         // (withheld: the consumers' waits run out)
+          const int k0 = (k * g.splits + split) * kBlockK;
+          const uint32_t bar = kCG == 2 ? mapa(full + 8 * s, 0) : full + 8 * s;
+          if (leader) mbar_expect(full + 8 * s, bytes * kCG);
+#pragma unroll
+          for (int p = 0; p < (kPlanes ? 3 : 1); ++p) {
+            const uint32_t sa = tiles + s * S::kStageBytes + p * S::kABytes, sb = tiles + s * S::kStageBytes + (kPlanes ? 3 : 1) * S::kABytes + p * S::kBBytes;
             if (g.a_rows_inner) {
-              tma_load<kCG>(sa, &map_a, a0, st.kb * kBlockK, st.pa, bar);
-              tma_load<kCG>(sa + 8192, &map_a, a0 + 64, st.kb * kBlockK, st.pa, bar);
+              tma_load<kCG>(sa, &map_a, a0, k0, p, bar);
+              tma_load<kCG>(sa + 8192, &map_a, a0 + 64, k0, p, bar);
             } else {
-              tma_load<kCG>(sa, &map_a, st.kb * kBlockK, a0, st.pa, bar);
+              tma_load<kCG>(sa, &map_a, k0, a0, p, bar);
             }
             if (g.b_rows_inner) {
 #pragma unroll
-              for (int c = 0; c < (S::kCols < 64 ? 1 : S::kCols / 64); ++c)
-                tma_load<kCG>(sb + c * 8192, &map_b, b0 + c * 64, st.kb * kBlockK, st.pb, bar);
+              for (int c = 0; c < (S::kCols < 64 ? 1 : S::kCols / 64); ++c) tma_load<kCG>(sb + c * 8192, &map_b, b0 + c * 64, k0, p, bar);
             } else {
-              tma_load<kCG>(sb, &map_b, st.kb * kBlockK, b0, st.pb, bar);
+              tma_load<kCG>(sb, &map_b, k0, b0, p, bar);
             }
           }
         }
@@ -296,24 +285,27 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       bool ok = true;
       for (int i = first; i < n_items && ok; i += stride) {
         const Item w = item_of(g, i, split);
-        const int seg = kPlanes ? kSegment : w.blocks;
+        const int seg = kPlanes ? 1 : w.blocks;          // blocks to an accumulator
         for (int k = 0; k < w.blocks && ok; k += seg, ++u) {
-          const int steps = min(seg, w.blocks - k) * (kPlanes ? kProducts : 1);
           ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(tempty + 8 * (u & 1u), ((u >> 1) & 1u) ^ 1u, limit));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t d = tmem + (u & 1u) * kBN;
-          for (int it = 0; it < steps; ++it, ++n) {
+          for (int it = 0; it < seg; ++it, ++n) {
             const uint32_t s = n % S::kStages;
             ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(full + 8 * s, (n / S::kStages) & 1u, limit));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t sa = tiles + s * S::kStageBytes;
-            const uint64_t da = umma_desc(sa, g.a_rows_inner), db = umma_desc(sa + S::kABytes, g.b_rows_inner);
+            const uint32_t sa = tiles + s * S::kStageBytes, sb = sa + (kPlanes ? 3 : 1) * S::kABytes;
             if (one) {
 #pragma unroll
-              for (int j = 0; j < kBlockK / 16; ++j)
-                umma<kCG>(d, da + (uint64_t)(j * adv_a), db + (uint64_t)(j * adv_b), idesc, it > 0 || j > 0);
+              for (int q = 0; q < (kPlanes ? kProducts : 1); ++q) {
+                const int pa = kPlanes ? (0x201100 >> (4 * (5 - q))) & 3 : 0, pb = kPlanes ? (0x021010 >> (4 * (5 - q))) & 3 : 0;
+                const uint64_t da = umma_desc(sa + pa * S::kABytes, g.a_rows_inner), db = umma_desc(sb + pb * S::kBBytes, g.b_rows_inner);
+#pragma unroll
+                for (int j = 0; j < kBlockK / 16; ++j)
+                  umma<kCG>(d, da + (uint64_t)(j * adv_a), db + (uint64_t)(j * adv_b), idesc, it > 0 || q > 0 || j > 0);
+              }
               umma_commit<kCG>(empty + 8 * s);
             }
             __syncwarp();
@@ -329,18 +321,18 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
   } else {
     const int quarter = warp & 3, half = warp >> 2;      // tensor memory lanes 32 quarter .. , columns half * kHalf ..
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    constexpr int kC = kPlanes ? 16 : S::kChunk, kChunks = kHalf / kC;
+    constexpr int kC = S::kChunk, kChunks = kHalf / kC;
     uint32_t u = 0;
     bool ok = true;
     Epilogue e;
-    e.in = tiles + S::kStages * S::kStageBytes + warp * 4 * S::kSlotBytes;
-    e.out = e.in + 2 * S::kSlotBytes;
+    e.out = tiles + S::kStages * S::kStageBytes + warp * (kPlanes ? 2 : 4) * S::kSlotBytes;
+    e.in = e.out + 2 * S::kSlotBytes;
     e.bar = smem_u32(s_in) + 16 * warp;
     e.asked = e.got = e.put = 0;
     for (int i = first; i < n_items && ok; i += stride) {
       const Item w = item_of(g, i, split);
       const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + half * kHalf;
-      const int seg = kPlanes ? kSegment : w.blocks;
+      const int seg = kPlanes ? 1 : w.blocks;
       // chunks that lie in D at all
       const int chunks = a0 < g.na && b0 < g.nb ? min(kChunks, (g.nb - b0 + kC - 1) / kC) : 0;
       // the residual's next chunk is asked for a chunk ahead, a tile's first while its sums are still being formed
@@ -410,7 +402,6 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           for (int j = 0; j < kC; ++j) x[j] = acc[c * kC + j];
           if (g.splits == 1) {
             if (c < chunks && ok) {
-              ask(c + 1);
               ok = finish_chunk<T, kC>(g, e, &map_out, &map_pre, x, bias, a0, b0 + c * kC, lane, limit);
             }
           } else {
@@ -481,10 +472,10 @@ cudaError_t allow_smem(K kernel, size_t bytes) {
 }
 template <typename T>
 cudaError_t allow_all() {
-  cudaError_t e = allow_smem(k_linear_tc<T, 256, 2>, Shape<256, 2>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 128, 1>, Shape<128, 1>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 64, 1>, Shape<64, 1>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 32, 1>, Shape<32, 1>::kSmem);
+  cudaError_t e = allow_smem(k_linear_tc<T, 256, 2>, Shape<T, 256, 2>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 128, 1>, Shape<T, 128, 1>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 64, 1>, Shape<T, 64, 1>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 32, 1>, Shape<T, 32, 1>::kSmem);
   return e;
 }
 template <typename K>
@@ -512,9 +503,9 @@ cudaError_t device_of(const Device** out) {
     if (tensor_map_encoder() == nullptr) return cudaErrorNotSupported;
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = allow_all<float>()) != cudaSuccess || (e = allow_all<__nv_bfloat16>()) != cudaSuccess || (e = allow_all<__half>()) != cudaSuccess) return e;
-    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<256, 2>::kSmem);
+    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<__nv_bfloat16, 256, 2>::kSmem);
     if (d.pairs < 1) return cudaErrorNotSupported;
-    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<128, 1>::kSmem);
+    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<__nv_bfloat16, 128, 1>::kSmem);
     d.known = true;
   }
   *out = &d;
@@ -535,13 +526,13 @@ bool encode_result(CUtensorMap* map, const Side& m, int na, int nb, int cols) {
 
 template <typename T, int kBN, int kCG>
 cudaError_t launch(const Planes& A, const Planes& B, TcArgs g, unsigned ctas, cudaStream_t s) {
-  using S = Shape<kBN, kCG>;
+  using S = Shape<T, kBN, kCG>;
   alignas(64) CUtensorMap ma, mb, mo = {}, mr = {}, mp = {};
   if (!encode_operand(&ma, A, g.bf16, kRows) || !encode_operand(&mb, B, g.bf16, S::kCols)) return cudaErrorInvalidValue;
-  constexpr int kC = sizeof(T) == 4 ? 16 : S::kChunk;
+  constexpr int kC = S::kChunk;
   if (g.splits == 1 && !S::kNarrow) {                    // (shared tiles are finished element by element)
     g.out_tma = encode_result<T>(&mo, g.f.out, g.na, g.nb, kC);
-    g.residual_tma = encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
+    g.residual_tma = !S::kPlanes && encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
     g.preact_tma = encode_result<T>(&mp, g.f.preact, g.na, g.nb, kC);
   }
   return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
