@@ -347,7 +347,7 @@ typedef struct { void* data; int64_t row_stride, col_stride; } strads_matrix_t;
 
 typedef struct {
   int32_t type, activation;             /* strads_type_t, strads_activation_t                     */
-  int64_t n_rows, n_in, n_out;          /* 0 <= n_rows < 2^31, 1 <= n_in, n_out < 2^31             */
+  int64_t n_rows, n_in, n_out;          /* 0 <= n_rows <= 2^30, 1 <= n_in, n_out <= 2^30           */
   strads_const_matrix_t x, w;
   float scale;
   uint32_t flags;

@@ -367,7 +367,8 @@ bool valid_out(const strads_matrix_t& m, int size, long long rows, long long col
 int check(const strads_linear_config_t& c) {
   if (c.type < STRADS_F32 || c.type > STRADS_F16 || c.activation < STRADS_ACT_IDENTITY || c.activation > STRADS_ACT_SILU) return STRADS_ERR_INVALID_ARG;
   if (c.n_rows < 0 || c.n_in < 1 || c.n_out < 1 || !std::isfinite(c.scale) || (c.flags & ~STRADS_LINEAR_FLAG_STALL) != 0) return STRADS_ERR_INVALID_ARG;
-  if (c.n_rows > 0x7fffffffll || c.n_in > 0x7fffffffll || c.n_out > 0x7fffffffll) return STRADS_ERR_UNSUPPORTED;
+  constexpr long long kMost = 1ll << 30;                 // (places of tiles, and what lies past the last, fit 32 bits)
+  if (c.n_rows > kMost || c.n_in > kMost || c.n_out > kMost) return STRADS_ERR_UNSUPPORTED;
   const int size = c.type == STRADS_F32 ? 4 : 2;
   if (!valid_in(c.w, size) || (c.n_rows > 0 && !valid_in(c.x, size))) return STRADS_ERR_INVALID_ARG;
   return STRADS_OK;

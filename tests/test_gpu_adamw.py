@@ -309,6 +309,22 @@ def test_on_another_stream(b):
     assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_two_to_the_31_elements(b, bits):
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 60 GB")
+    n = (1 << 31) + 1000
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = [0, 5, (1 << 31) - 1, 1 << 31, (1 << 31) + 257, n - 1]
+    g[at] = 1.0
+    opt = b.AdamW([p], bits=bits)
+    opt.step([g], lr=0.5, step=1)
+    want = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    want[at] = -0.5                                      # the first step's length is lr, to 1e-8
+    assert torch.equal(p, want)
+
+
 def test_the_class_refuses(b):
     p = torch.randn(100, device="cuda")
     g = torch.randn(100, device="cuda")

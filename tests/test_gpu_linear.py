@@ -8,6 +8,8 @@ result is rounded to its type: eps / 2 relative, and half a subnormal step of bi
 to the type where the products read it: eps / 2 of S more.
 """
 import math
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -282,6 +284,56 @@ def test_same_bits_every_time(b, dtype, shape):
     x, w, g = matrix(n, k, dtype, gen), matrix(m, k, dtype, gen), matrix(n, m, dtype, gen)
     runs = [[b.linear_forward(x, w), *b.linear_backward(g, x, w)] for _ in range(3)]
     assert all(torch.equal(p, q) for r in runs[1:] for p, q in zip(r, runs[0]))
+
+
+def test_offsets_past_32_bits(b):
+    """A weight of 2.8 G elements, by one row, by twenty, and its gradient; spots of the results against 64 bits."""
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("needs 40 GB")
+    m, k = 70_000, 40_000
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    w = torch.empty(m, k, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    x = matrix(20, k, torch.bfloat16, gen)
+    rows = torch.tensor([0, 1, 53_686, 53_687, 53_688, 69_998, 69_999], device="cuda")      # 2^31 / k = 53,687.1
+    for n in (1, 20):
+        out = b.linear_forward(x[:n], w)
+        z64 = x[:n].to(F64) @ w[rows].to(F64).t()
+        s = (k + 16) * 2.0 ** -24 * (x[:n].to(F64).abs() @ w[rows].to(F64).abs().t())
+        close(out[:, rows], z64, s + half_step(z64.abs() + s, torch.bfloat16))
+        g = matrix(n, m, torch.bfloat16, gen)
+        _, gw, gb = b.linear_backward(g, x[:n], w, want_x=False, grad_w=w.new_empty(m, k))
+        want = g[:, rows].to(F64).t() @ x[:n].to(F64)
+        tol = (n + 16) * 2.0 ** -24 * (g[:, rows].to(F64).abs().t() @ x[:n].to(F64).abs())
+        close(gw[rows], want, tol + half_step(want.abs() + tol, torch.bfloat16))
+        # the same weight in the order of its columns: rows of x run through memory
+        gt, xt = w.view(-1)[: n * m].view(m, n).t(), w.view(-1)[-n * k:].view(n, k)
+        out = b.linear_forward(gt, xt.new_ones(3, m))
+        assert torch.isfinite(out).all()
+        del gw
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_the_first_call_of_a_process_may_be_captured(n):
+    code = f"""
+import sys, torch
+from paper_1312_5766_b200 import binding as b
+x, w = torch.randn({n}, 512, device="cuda").bfloat16(), torch.randn(256, 512, device="cuda").bfloat16()
+p, g = torch.randn(1000, device="cuda"), torch.randn(1000, device="cuda")
+opt = b.AdamW([p])
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = b.linear_forward(x, w, activation="gelu")
+    grads = b.linear_backward(out, x, w)
+    opt.step([g], step=1)
+q = p.clone()
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, b.linear_forward(x, w, activation="gelu"))
+assert all(torch.equal(s, t) for s, t in zip(grads, b.linear_backward(out, x, w)))
+assert not torch.equal(p, q)
+"""
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
 
 
 def test_gradients_against_differences(b):

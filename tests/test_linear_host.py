@@ -51,7 +51,7 @@ def test_bad_operands(b, which):
         for side in "xw":
             assert _call(b, _config(b, **{side: x.data, side + "_row_stride": x.row_stride, side + "_col_stride": x.col_stride}), which) == -1
     for n in ("n_rows", "n_in", "n_out"):
-        assert _call(b, _config(b, **{n: 1 << 31}), which) == -7
+        assert _call(b, _config(b, **{n: (1 << 30) + 1}), which) == -7
 
 
 def test_bad_outputs(b):
