@@ -12,40 +12,56 @@ __device__ unsigned int g_linear_status;       // STRADS_STATUS_* bits of the la
 constexpr int kThreads = 256;
 
 // ---- operands of the tensor-core products that cannot be read in place ----
-// dst[plane][outer][ld] from src, eight neighbours per thread; binary32 as three planes of bfloat16 (split_pair).
+// dst[plane][outer][ld] from src, eight neighbours per thread; binary32 as three planes of bfloat16 (split_pair).  All operands of a call that
+// need it in one launch.
+struct Copy {
+  const void* src;
+  long long outer_stride, inner_stride, outer, inner, ld, plane;
+  unsigned short* dst;
+  int vec;
+};
+constexpr int kMostCopies = 3;
+struct Copies { Copy c[kMostCopies]; int n; long long groups; };
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_linear_pack(const T* src, long long outer_stride, long long inner_stride, long long outer, long long inner,
-                                                          unsigned short* dst, long long ld, long long plane, int vec) {
+__device__ __forceinline__ void copy_group(const Copy& c, long long i) {
+  const long long per = c.ld / 8, o = i / per, k = i % per * 8;
+  const T* at = static_cast<const T*>(c.src) + o * c.outer_stride + k * c.inner_stride;
+  __align__(16) T x[8];
+  if (c.vec && k + 8 <= c.inner) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(x)[j] = __ldg(reinterpret_cast<const uint4*>(at) + j);
+  } else {
+    const long long last = c.inner - 1 - k;              // (clamped, not branched: all loads under way at once)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = at[(j < last ? j : last) * c.inner_stride];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) if (j > last) store_f32(&x[j], 0.f);
+  }
+  unsigned short* to = c.dst + o * c.ld + k;
+  if (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
+  } else {
+    __align__(16) uint32_t p[3][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t w[3];
+      split_pair(load_f32(&x[2 * j]), load_f32(&x[2 * j + 1]), w);
+      p[0][j] = w[0]; p[1][j] = w[1]; p[2][j] = w[2];
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + q * c.plane) = *reinterpret_cast<const uint4*>(p[q]);
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_linear_pack(const __grid_constant__ Copies all) {
   chain_begin();
-  const long long per = ld / 8, total = outer * per;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < total; i += (long long)gridDim.x * kThreads) {
-    const long long o = i / per, k = i % per * 8;
-    const T* at = src + o * outer_stride + k * inner_stride;
-    __align__(16) T x[8];
-    if (vec && k + 8 <= inner) {
-#pragma unroll
-      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(x)[j] = __ldg(reinterpret_cast<const uint4*>(at) + j);
-    } else {
-      const long long last = inner - 1 - k;              // (< 0: a group of padding alone; clamped, not branched: all loads under way at once)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = at[(j < last ? j : last) * inner_stride];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) if (j > last) store_f32(&x[j], 0.f);
-    }
-    unsigned short* to = dst + o * ld + k;
-    if (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(x);
-    } else {
-      __align__(16) uint32_t p[3][4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t w[3];
-        split_pair(load_f32(&x[2 * j]), load_f32(&x[2 * j + 1]), w);
-        p[0][j] = w[0]; p[1][j] = w[1]; p[2][j] = w[2];
-      }
-#pragma unroll
-      for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(to + q * plane) = *reinterpret_cast<const uint4*>(p[q]);
-    }
+  // the groups of all matrices as one run, so that a thread's loads do not wait for those of another matrix
+  const long long stride = (long long)gridDim.x * kThreads;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all.groups; i += stride) {
+    long long at = i;
+    int n = 0;
+    while (n + 1 < all.n && at >= all.c[n].plane / 8) at -= all.c[n++].plane / 8;
+    copy_group<T>(all.c[n], at);
   }
 }
 
@@ -153,6 +169,7 @@ struct Call {
   cudaStream_t stream;
   cudaError_t err;
   unsigned int* status;
+  Copies copies;                         // to be made before the next product
   void* take(size_t bytes) {
     void* p = ws + used;
     used += (bytes + 255) / 256 * 256;
@@ -188,13 +205,20 @@ Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unkno
   if (unknown && p.inner * ((p.outer + 7) / 8 * 8) > p.plane) p.plane = p.inner * ((p.outer + 7) / 8 * 8);      // (either order)
   void* dst = c.take((size_t)p.plane * p.planes * 2);
   p.p = dst;
-  if (!c.run || c.err != cudaSuccess) return p;
-  const int vec = (inner_stride == 1) && vec_rows(m.p, outer_stride, p.outer, c.size);
-  const unsigned grid = ctas_for(p.plane / 8);
-  unsigned short* to = static_cast<unsigned short*>(dst);
-  c.err = c.size == 4 ? launch_chained(k_linear_pack<float>, grid, kThreads, 0, c.stream, static_cast<const float*>(m.p), outer_stride, inner_stride, p.outer, p.inner, to, p.ld, p.plane, vec)
-                      : launch_chained(k_linear_pack<__half>, grid, kThreads, 0, c.stream, static_cast<const __half*>(m.p), outer_stride, inner_stride, p.outer, p.inner, to, p.ld, p.plane, vec);
+  if (!c.run) return p;
+  c.copies.c[c.copies.n++] = {m.p, outer_stride, inner_stride, p.outer, p.inner, p.ld, p.plane, static_cast<unsigned short*>(dst),
+                              inner_stride == 1 && vec_rows(m.p, outer_stride, p.outer, c.size)};
   return p;
+}
+// The copies asked for so far, in one launch.
+void copy(Call& c) {
+  if (!c.run || c.err != cudaSuccess || c.copies.n == 0) return;
+  c.copies.groups = 0;
+  for (int i = 0; i < c.copies.n; ++i) c.copies.groups += c.copies.c[i].plane / 8;
+  const unsigned grid = ctas_for(c.copies.groups);
+  c.err = c.size == 4 ? launch_chained(k_linear_pack<float>, grid, kThreads, 0, c.stream, c.copies)
+                      : launch_chained(k_linear_pack<__half>, grid, kThreads, 0, c.stream, c.copies);
+  c.copies.n = 0;
 }
 
 // A matrix as one side of products, brought into the workspace at most once: the other side of its transpose is the same copy.
@@ -218,28 +242,49 @@ Planes side_of(Call& c, Matrix& x, bool columns_as_rows) {
   return p;
 }
 
-// D = A B^T, A and B matrices or (t) their transposes.
-void product(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
-  const Operand a = ta ? Operand{A.m.p, A.m.ks, A.m.rs} : A.m, b = tb ? Operand{B.m.p, B.m.ks, B.m.rs} : B.m;
-  const long long na = ta ? A.cols : A.rows, nb = tb ? B.cols : B.rows, nk = ta ? A.rows : A.cols;
-  if ((na < nb ? na : nb) <= kThinMost) {
-    if (c.run && c.err == cudaSuccess) c.err = launch_linear_thin(c.type, a, b, na, nb, nk, f, c.stream);
-    return;
-  }
+// D = A B^T, A and B matrices or (t) their transposes: which kernel forms it, and its operands as that reads them.
+struct Product {
+  enum Way { kNone, kThin, kSplit, kTensor } way;
+  Operand a, b;
+  long long na, nb, nk;
+  Planes pa, pb;
+  void* ws;
+  bool b_long;
+  Finish f;
+};
+Product plan(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
+  Product d = {};
+  d.a = ta ? Operand{A.m.p, A.m.ks, A.m.rs} : A.m;
+  d.b = tb ? Operand{B.m.p, B.m.ks, B.m.rs} : B.m;
+  d.na = ta ? A.cols : A.rows; d.nb = tb ? B.cols : B.rows; d.nk = ta ? A.rows : A.cols;
+  d.f = f;
+  d.way = Product::kThin;
+  if ((d.na < d.nb ? d.na : d.nb) <= kThinMost) return d;
   // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 32 or 48
   // rows, most of them from L2, where planes in memory cost 16)
-  const bool b_long = na < nb || (na == nb && B.order < A.order);
-  const Operand &l = b_long ? b : a, &sh = b_long ? a : b;
-  const long long nl = b_long ? nb : na, ns = b_long ? na : nb;
-  const bool unknown = (b_long ? B : A).unknown;         // (a query: room for either way)
-  if (c.size == 4 && ns <= kSplitMost && (unknown || linear_split_takes(l, nl, nk))) {
-    const Planes p = bring(c, sh, ns, nk, false, true);
-    void* ws = c.take(linear_split_workspace(nl, ns, nk));
-    if (c.run && c.err == cudaSuccess) c.err = launch_linear_split(l, p, nl, ns, nk, b_long, f, ws, c.status, c.stall, c.stream);
-    if (!unknown) return;
+  d.b_long = d.na < d.nb || (d.na == d.nb && B.order < A.order);
+  const Operand &l = d.b_long ? d.b : d.a, &sh = d.b_long ? d.a : d.b;
+  const long long nl = d.b_long ? d.nb : d.na, ns = d.b_long ? d.na : d.nb;
+  const bool unknown = (d.b_long ? B : A).unknown;       // (a query: room for either way)
+  if (c.size == 4 && ns <= kSplitMost && (unknown || linear_split_takes(l, nl, d.nk))) {
+    d.way = Product::kSplit;
+    d.pb = bring(c, sh, ns, d.nk, false, true);
+    d.ws = c.take(linear_split_workspace(nl, ns, d.nk));
+    if (!unknown) return d;
   }
-  const Planes pa = side_of(c, A, ta), pb = side_of(c, B, tb);
-  if (c.run && c.err == cudaSuccess) c.err = launch_linear_tc(c.type, pa, pb, na, nb, nk, f, c.status, c.stall, c.stream);
+  d.way = Product::kTensor;
+  d.pa = side_of(c, A, ta);
+  d.pb = side_of(c, B, tb);
+  return d;
+}
+void launch(Call& c, const Product& d) {
+  if (!c.run || c.err != cudaSuccess || d.way == Product::kNone) return;
+  if (d.way == Product::kThin)
+    c.err = launch_linear_thin(c.type, d.a, d.b, d.na, d.nb, d.nk, d.f, c.stream);
+  else if (d.way == Product::kSplit)
+    c.err = launch_linear_split(d.b_long ? d.b : d.a, d.pb, d.b_long ? d.nb : d.na, d.b_long ? d.na : d.nb, d.nk, d.b_long, d.f, d.ws, c.status, c.stall, c.stream);
+  else
+    c.err = launch_linear_tc(c.type, d.pa, d.pb, d.na, d.nb, d.nk, d.f, c.status, c.stall, c.stream);
 }
 
 Side side(const void* p, long long rs, long long cs, bool a_is_rows) { return a_is_rows ? Side{p, rs, cs} : Side{p, cs, rs}; }
@@ -260,7 +305,9 @@ void forward(Call& c, const strads_linear_config_t& g, const void* bias, const s
   if (preact) f.preact = side(preact->data, preact->row_stride, preact->col_stride, ar);
   f.bias_a = ar ? 0 : 1; f.bias_b = ar ? 1 : 0;
   f.plain = g.activation == STRADS_ACT_IDENTITY && bias == nullptr && residual == nullptr && preact == nullptr;
-  if (ar) product(c, x, false, w, false, f); else product(c, w, false, x, false, f);
+  const Product d = ar ? plan(c, x, false, w, false, f) : plan(c, w, false, x, false, f);
+  copy(c);
+  launch(c, d);
 }
 
 template <typename T>
@@ -317,16 +364,20 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
   Finish f = {};
   f.plain = 1;
   f.scale = formed ? 1.f : g.scale;
+  Product dx = {}, dw = {};
   if (gx != nullptr || c.all) {
     const bool ar = gx != nullptr && rows_run(gx->row_stride, gx->col_stride);
     if (gx != nullptr) f.out = side(gx->data, gx->row_stride, gx->col_stride, ar);
-    if (ar) product(c, z, false, w, true, f); else product(c, w, true, z, false, f);
+    dx = ar ? plan(c, z, false, w, true, f) : plan(c, w, true, z, false, f);
   }
   if (gw != nullptr || c.all) {
     const bool ar = gw != nullptr && rows_run(gw->row_stride, gw->col_stride);
     if (gw != nullptr) f.out = side(gw->data, gw->row_stride, gw->col_stride, ar);
-    if (ar) product(c, z, true, x, true, f); else product(c, x, true, z, true, f);
+    dw = ar ? plan(c, z, true, x, true, f) : plan(c, x, true, z, true, f);
   }
+  copy(c);
+  launch(c, dx);
+  launch(c, dw);
 }
 void backward_of(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, const strads_matrix_t* gx,
                  const strads_matrix_t* gw, void* gbias) {
