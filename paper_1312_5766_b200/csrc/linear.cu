@@ -280,7 +280,7 @@ Product plan(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
 void launch(Call& c, const Product& d) {
   if (!c.run || c.err != cudaSuccess || d.way == Product::kNone) return;
   if (d.way == Product::kThin)
-    c.err = launch_linear_thin(c.type, d.a, d.b, d.na, d.nb, d.nk, d.f, c.stream);
+    c.err = launch_linear_thin(c.type, d.a, d.b, d.na, d.nb, d.nk, d.f, c.status, c.stall, c.stream);
   else if (d.way == Product::kSplit)
     c.err = launch_linear_split(d.b_long ? d.b : d.a, d.pb, d.b_long ? d.nb : d.na, d.b_long ? d.na : d.nb, d.nk, d.b_long, d.f, d.ws, c.status, c.stall, c.stream);
   else

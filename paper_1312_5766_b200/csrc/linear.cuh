@@ -142,6 +142,7 @@ __device__ __forceinline__ void finish(const Finish& f, float z, long long a, lo
 // ---- products with few rows on one side (linear_thin.cu) ----
 // D = A B^T with at most kThinMost rows in B, or in A (then swapped): every element of the long side is read once, from where it is.
 constexpr int kThinMost = 4;
-cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s);
+cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, unsigned int* status,
+                               bool stall, cudaStream_t s);
 
 }  // namespace strads

@@ -3,8 +3,9 @@
 // cores: a tile of theirs would be nearly empty, and binary32 would have to be split first.
 //
 //   k along memory (k_thin_k): a warp takes rows, a lane every 32nd group of 16 bytes of them; lanes are added by shuffles.
-//   rows along memory (k_thin_rows): a lane takes the rows of 16 bytes (or of 4, where there are few), a warp every 16th k; warps
-//   are added through shared memory.
+//   rows along memory (k_thin_tiles): tiles of 512 bytes of rows by 32 k come by TMA into a ring, a lane takes the rows of 16 bytes, a warp every
+//   eighth k; warps are added through shared memory.  What TMA cannot address goes by k_thin_rows: the same without the ring, a lane the rows of 16
+//   bytes (or of 4, where there are few).
 //
 // What hides the memory's latency is the number of loads under way: four or eight per lane, and as many warps as that leaves registers for (rows along
 // memory, 10,000 x 100,000 binary32: 767 us with 4 a lane, 833 with 8, 2,280 with 16 and half the warps); where the rows alone do not
@@ -12,7 +13,8 @@
 // The short side is staged in shared memory as binary32, or (k along memory, up to four rows) read through L1 as it is.
 #include <mutex>
 
-#include "linear.cuh"
+#include "linear_tc.cuh"
+#include "linear_ptx.cuh"
 
 namespace strads {
 namespace {
@@ -25,19 +27,17 @@ struct Thin {
   long long nl, nk;
   int ns, splits, swapped, vec, svec;          // swapped: the long side is D's b; vec, svec: 16-byte accesses to the long, the short side
   int wk;                                      // k_thin_k: warps of a CTA that share a row's k (1 or 8)
+  int stall;
+  unsigned int* status;
   Finish f;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ float load_peer(const float* p, uint32_t rank) {
   uint32_t a;
   float v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
   return v;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 template <typename T>
 __device__ __forceinline__ void finish_thin(const Thin& t, float v, long long l, int s) {
@@ -274,6 +274,113 @@ __global__ void __launch_bounds__(kRowThreads) k_thin_rows(const __grid_constant
   if (t.splits > 1) cluster_sync();
 }
 
+// ---- rows along memory, by TMA ----
+constexpr int kTileK = 32, kTileBytes = 512 * kTileK, kTileStages = 6, kTileWarps = 8;
+constexpr size_t kTileSmem = (size_t)kTileStages * kTileBytes + 1024;
+template <typename T, int kT>
+__global__ void __launch_bounds__(32 * (kTileWarps + 1), 2) k_thin_tiles(const __grid_constant__ CUtensorMap map, const __grid_constant__ Thin t) {
+  constexpr int kV = 16 / sizeof(T), kTile = 32 * kV, kSums = kT * kTile, kRows = kTileK / kTileWarps;
+  extern __shared__ unsigned char dyn[];
+  __shared__ __align__(8) uint64_t s_full[kTileStages], s_empty[kTileStages];
+  __shared__ float sum[kSums];
+  __shared__ volatile int s_abort;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t ring = (smem_u32(dyn) + 127u) & ~127u, full = smem_u32(s_full), empty = smem_u32(s_empty);
+  const uint32_t limit = t.stall ? kMmaStallLimit : kMmaWaitLimit;
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int i = 0; i < kTileStages; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, kTileWarps); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+  }
+  __syncthreads();
+  chain_begin();
+  const long long l0 = (long long)(blockIdx.x / t.splits) * kTile;
+  const int rank = t.splits > 1 ? (int)(blockIdx.x % t.splits) : 0;
+  // blocks of 32 k of this CTA: rank, rank + splits, ..
+  const int blocks = (int)((t.nk + kTileK - 1) / kTileK), mine = (blocks - rank + t.splits - 1) / t.splits;
+  bool ok = true;
+  float acc[kT][kV] = {};
+  if (warp == kTileWarps) {
+    if (elect_one()) {
+      int n = 0;
+      for (; n < mine; ++n) {
+        const uint32_t s = (uint32_t)(n % kTileStages);
+        ok = !s_abort && mbar_wait(empty + 8 * s, ((uint32_t)(n / kTileStages) & 1u) ^ 1u, limit) && !t.stall;
+        if (!ok) break;
+        mbar_expect(full + 8 * s, (uint32_t)kTileBytes);
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(ring + s * kTileBytes), "l"(&map), "r"((int)l0), "r"((rank + n * t.splits) * kTileK), "r"(full + 8 * s) : "memory");
+      }
+      // nothing is under way when the shared memory goes
+      for (int j = n > kTileStages ? n - kTileStages : 0; j < n; ++j)
+        if (!mbar_wait(full + 8 * (uint32_t)(j % kTileStages), (uint32_t)(j / kTileStages) & 1u, limit)) { ok = false; break; }
+      if (!ok) { s_abort = 1; atomicOr(t.status, STRADS_STATUS_WAIT_EXPIRED); }
+    }
+    __syncwarp();
+  } else {
+    // the short side's values of this warp's rows of a block: lane r * kT + s holds that of row r; a block ahead
+    const int r = lane / kT, sr = lane % kT;
+    auto fetch = [&](int n) {
+      const long long k = (long long)(rank + n * t.splits) * kTileK + warp * kRows + r;
+      return r < kRows && sr < t.ns && n < mine && k < t.nk ? load_f32(static_cast<const T*>(t.S.p) + sr * t.S.rs + k * t.S.ks) : 0.f;
+    };
+    float held = fetch(0);
+    for (int n = 0; n < mine; ++n) {
+      const float now = held;
+      held = fetch(n + 1);
+      const uint32_t s = (uint32_t)(n % kTileStages);
+      ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(full + 8 * s, (uint32_t)(n / kTileStages) & 1u, limit));
+      if (!ok) break;
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        uint4 raw;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w)
+                     : "r"(ring + s * kTileBytes + (warp * kRows + i) * 512 + lane * 16) : "memory");
+        Raw<16> w;
+        w.v = raw;
+        float x[kV];
+        to_floats<T, 16>(w, x);
+#pragma unroll
+        for (int q = 0; q < kT; ++q) {
+          const float y = __shfl_sync(0xffffffffu, now, i * kT + q);
+#pragma unroll
+          for (int v = 0; v < kV; ++v) acc[q][v] = fmaf(x[v], y, acc[q][v]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(empty + 8 * s) : "memory");
+    }
+    if (!ok && lane == 0) { s_abort = 1; atomicOr(t.status, STRADS_STATUS_WAIT_EXPIRED); }
+  }
+  __syncthreads();                                       // (all of the ring has been read: the warps' sums take its place)
+  float* part = reinterpret_cast<float*>(dyn);
+  if (warp < kTileWarps)
+#pragma unroll
+    for (int q = 0; q < kT; ++q)
+#pragma unroll
+      for (int v = 0; v < kV; ++v) part[warp * kSums + q * kTile + v * 32 + lane] = acc[q][v];
+  __syncthreads();
+  for (int i = threadIdx.x; i < kSums; i += 32 * (kTileWarps + 1)) {
+    float a = part[i];
+#pragma unroll
+    for (int w = 1; w < kTileWarps; ++w) a += part[w * kSums + i];
+    sum[i] = a;
+  }
+  if (t.splits > 1) cluster_sync(); else __syncthreads();
+  if (!s_abort)
+    for (int i = rank * 32 * (kTileWarps + 1) + threadIdx.x; i < kSums; i += 32 * (kTileWarps + 1) * t.splits) {
+      const int q = i / kTile, j = i % kTile;
+      if (l0 + j >= t.nl || q >= t.ns) continue;
+      const float* p = sum + q * kTile + (j % kV) * 32 + j / kV;
+      float v = 0.f;
+      if (t.splits == 1) v = *p;
+      else for (int c = 0; c < t.splits; ++c) v += load_peer(p, (uint32_t)c);
+      finish_thin<T>(t, v, l0 + j, q);
+    }
+  if (t.splits > 1) cluster_sync();
+}
+
 bool vec_ok(const void* p, long long pitch, long long rows, size_t size) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || (pitch * (long long)size) % 16 == 0); }
 
 template <typename T, int kT, int kBytes>
@@ -288,6 +395,26 @@ cudaError_t launch_rows(const Thin& t, long long tiles, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   return launch_chained_cluster(k_thin_rows<T, kT, kBytes>, dim3((unsigned)(tiles * t.splits)), kRowThreads, kSmem, s, t.splits, t);
+}
+template <typename T, int kT>
+cudaError_t launch_tiles(Thin t, int sms, cudaStream_t s) {
+  constexpr int kTile = 512 / (int)sizeof(T);
+  const long long tiles = (t.nl + kTile - 1) / kTile, blocks = (t.nk + kTileK - 1) / kTileK;
+  // as many CTAs to a tile as leave all of them resident, two to an SM, with four blocks each at least
+  t.splits = 1;
+  for (int n = 2; n <= 16; ++n)
+    if (tiles * n <= 2ll * sms && blocks >= 4ll * n) t.splits = n;
+  alignas(64) CUtensorMap map;
+  const cuuint64_t dims[2] = {(cuuint64_t)t.nl, (cuuint64_t)t.nk}, strides[1] = {(cuuint64_t)t.L.ks * sizeof(T)};
+  const cuuint32_t box[2] = {(cuuint32_t)kTile, (cuuint32_t)kTileK}, estr[2] = {1, 1};
+  if (tensor_map_encoder()(&map, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(t.L.p), dims, strides, box,
+                           estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(k_thin_tiles<T, kT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTileSmem);
+  if (e == cudaSuccess && t.splits > 8) e = cudaFuncSetAttribute(k_thin_tiles<T, kT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  return launch_chained_cluster(k_thin_tiles<T, kT>, dim3((unsigned)(tiles * t.splits)), 32 * (kTileWarps + 1), kTileSmem, s, t.splits, map, t);
 }
 template <typename T, int kT>
 cudaError_t launch(Thin t, int sms, cudaStream_t s) {
@@ -306,6 +433,7 @@ cudaError_t launch(Thin t, int sms, cudaStream_t s) {
     return launch_chained_cluster(k_thin_k<T, kT, kR, false>, grid, kThreads, 0, s, t.splits, t);
   }
   t.vec = vec_ok(t.L.p, t.L.ks, t.nk, sizeof(T));
+  if (t.vec && t.nk > 1 && t.L.ks >= t.nl && tensor_map_encoder() != nullptr) return launch_tiles<T, kT>(t, sms, s);
   // 16 bytes of a row per lane where that leaves enough CTAs, 4 otherwise; then as many CTAs to a tile as keep four on every SM
   const long long wide = (t.nl + 512 / (int)sizeof(T) - 1) / (512 / (int)sizeof(T)), narrow = (t.nl + 128 / (int)sizeof(T) - 1) / (128 / (int)sizeof(T));
   const bool few = wide * 32 < sms;
@@ -320,13 +448,14 @@ cudaError_t by_short(const Thin& t, int sms, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, cudaStream_t s) {
+cudaError_t launch_linear_thin(int type, const Operand& A, const Operand& B, long long na, long long nb, long long nk, const Finish& f, unsigned int* status,
+                               bool stall, cudaStream_t s) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   Thin t = {};
-  t.f = f; t.nk = nk;
+  t.f = f; t.nk = nk; t.status = status; t.stall = stall;
   t.swapped = na < nb;
   t.L = t.swapped ? B : A; t.S = t.swapped ? A : B;
   t.nl = t.swapped ? nb : na; t.ns = (int)(t.swapped ? na : nb);

@@ -358,10 +358,16 @@ def test_gradients_against_differences(b):
             assert abs((f[0] - f[1]) * 32 - float(terms.sum())) <= 1e-3 * float(terms.abs().sum())
 
 
-def test_a_wait_that_runs_out_is_reported(b):
-    """Operand loads withheld: the call ends after milliseconds, the status says so once, and the next call is right."""
+STALLS = [(300, 512, 256, torch.bfloat16, "rows"), (40, 2000, 300, torch.float16, "cols"), (4096, 512, 4096, torch.bfloat16, "rows"), (300, 900, 200, torch.float32, "rows"),
+          (1000, 2000, 1, torch.float32, "cols"), (1000, 2000, 3, torch.bfloat16, "cols"), (900, 1000, 20, torch.float32, "cols"), (900, 1000, 40, torch.float32, "rows")]
+
+
+@pytest.mark.parametrize("n,k,m,dtype,order", STALLS, ids=str)
+def test_a_wait_that_runs_out_is_reported(b, n, k, m, dtype, order):
+    """Operand loads withheld, in every kernel that waits for some: the call ends after milliseconds, the status says so once, and the next
+    call is right."""
     gen = torch.Generator(device="cuda").manual_seed(4)
-    x, w = matrix(300, 512, torch.bfloat16, gen), matrix(256, 512, torch.bfloat16, gen)
+    x, w = matrix(n, k, dtype, gen, order), matrix(m, k, dtype, gen)
     assert b.linear_status() == (0, 0)
     want = b.linear_forward(x, w)
     b.linear_forward(x, w, flags=b.LINEAR_FLAG_STALL)
