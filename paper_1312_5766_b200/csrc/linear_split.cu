@@ -10,9 +10,11 @@
 //   L0 [S0 S1 S2] -> [c0 c1 c2],   L1 [S0 S1] -> [c1 c2],   L2 [S0] -> [c2],   D = c0 + (c1 + c2).
 // Four warps empty them into registers every kSegment blocks (the tensor cores' additions truncate) and add there.
 //
-// The blocks of all tiles, one tile after another, are dealt out evenly: every CTA takes a run of them, so that all SMs finish together
-// however the tiles divide.  A tile that falls to more than one CTA is left as partial sums in the workspace and finished by a second kernel, in the
-// order of the CTAs.  Waits are bounded as in linear_tc.cu.
+// Every CTA has the same number of blocks, however the tiles divide.  With W CTAs, each first takes whole tiles, the CTAs' tiles side by side; of the R
+// tiles left, CTAs 0 .. R - 1 take n1 = R B / W of the B blocks of one each, spread evenly over k, and the other W - R what is left of them.  So at any
+// time the CTAs read the same few k of neighbouring rows: runs of blocks of one tile after another, each CTA at a k of its own, read a column-major design
+// at 5.1 TB/s, where tiles in step reach 6.5.  The tiles shared are left as partial sums in the workspace and finished by a second kernel, in a
+// fixed order.  Waits are bounded as in linear_tc.cu.
 #include "linear_tc.cuh"
 #include "linear_ptx.cuh"
 
@@ -38,16 +40,19 @@ struct Sizes {
 
 struct SplitArgs {
   int nl, ns, blocks, tiles_l, tiles_s, ctas;
+  int rounds, shared, own;               // whole tiles of each CTA; R; n1
   int l_rows_inner, long_is_b, stall;
-  float* partial;                        // [2 ctas][kBN][128]
+  float* partial;                        // [ctas + R][kBN][128]
   unsigned int* status;
   Finish f;
 };
 
-// Blocks [first, last) of the whole run of tiles that CTA c takes.
-__device__ __forceinline__ long long start_of(const SplitArgs& g, int c) { return (long long)g.tiles_l * g.tiles_s * g.blocks * c / g.ctas; }
 // Tiles of one part of the long side follow each other: the second finds it in L2.
 __device__ __forceinline__ void tile_of(const SplitArgs& g, int t, int* tl, int* ts) { *tl = t / g.tiles_s; *ts = t % g.tiles_s; }
+// What the first R CTAs leave of the shared tiles, one tile after another: helper h takes [start, start of h + 1).
+__host__ __device__ __forceinline__ long long helper_start(const SplitArgs& g, int h) {
+  return (long long)g.shared * (g.blocks - g.own) * h / (g.ctas - g.shared);
+}
 // Columns s, s + 1, .. of row l (clamped to one that exists; `here`: it does).
 template <int kN>
 __device__ __forceinline__ void finish_split(const SplitArgs& g, float (&v)[kN], long long l, int s) {
@@ -65,11 +70,63 @@ __device__ __forceinline__ void finish_split(const SplitArgs& g, float (&v)[kN],
     finish_run<float, kN>(f, v, at, s, 1, count, here);
   }
 }
-// Counts through the blocks of a run: tile and block of k.
+// A CTA's blocks, piece by piece: a piece is some or all blocks of one tile.
 struct Walk {
-  int tile, block;
-  __device__ __forceinline__ Walk(const SplitArgs& g, long long u) : tile((int)(u / g.blocks)), block((int)(u % g.blocks)) {}
-  __device__ __forceinline__ void next(const SplitArgs& g) { if (++block == g.blocks) { block = 0; ++tile; } }
+  int round, tile, len, at;              // at: blocks of the piece gone through
+  int slot;                              // where its sums go (-1: it has the whole tile)
+  long long rest, from, end;             // helpers: where they are in what is left of the shared tiles; the piece's first block there; their end
+  __device__ __forceinline__ Walk(const SplitArgs& g, int c) : round(-1), rest(0), end(0) {
+    if (c >= g.shared) { rest = helper_start(g, c - g.shared); end = helper_start(g, c - g.shared + 1); }
+    next_piece(g, c);
+  }
+  __device__ __forceinline__ void next_piece(const SplitArgs& g, int c) {      // len 0: no more
+    ++round;
+    at = 0;
+    if (round < g.rounds) {
+      tile = round * g.ctas + c; len = g.blocks; slot = -1;
+    } else if (c < g.shared) {
+      len = round == g.rounds ? g.own : 0;
+      tile = g.rounds * g.ctas + c; slot = g.own == g.blocks ? -1 : c;
+    } else if (rest < end) {
+      const int left = g.blocks - g.own, t = (int)(rest / left);
+      from = rest - (long long)t * left;
+      len = (int)min((long long)left - from, end - rest);
+      tile = g.rounds * g.ctas + t; slot = g.shared + t + (c - g.shared);
+      rest += len;
+    } else {
+      len = 0;
+    }
+  }
+};
+// Which of a tile's blocks a piece has, one after the other.  k along memory: the first n1 are dealt out first, and what follows is what is left, so that a
+// CTA reads on in its rows (10,000 x 100,000 by 20: 675 us, 780 spread).  Rows along memory: the i-th of the n1 is floor(i B / n1); of the others, the one
+// that as many of them precede: where a piece begins by division, from there on by counting.
+struct Order {
+  int k, step, rem, own, next, err;      // the block; floor(B / n1) and what it leaves; the next of the n1, and the remainder there
+  bool whole, first;
+  __device__ __forceinline__ Order(const SplitArgs& g, const Walk& w, int c) : k(0), step(1), rem(0), own(g.own), next(0), err(0), whole(w.slot < 0 || !g.l_rows_inner), first(c < g.shared) {
+    if (w.slot >= 0 && !g.l_rows_inner && !first) k = own + (int)w.from;
+    if (whole || w.len == 0) return;
+    step = g.blocks / own; rem = g.blocks % own;
+    if (first) return;
+    const long long B = g.blocks, n1 = own, i = w.from + 1;
+    long long m = i * B / (B - n1);                      // m - ceil(m n1 / B) of the first m blocks are among the others: the least m with i of them
+    while (m - (m * n1 + B - 1) / B < i) ++m;
+    while (m > 1 && m - 1 - ((m - 1) * n1 + B - 1) / B >= i) --m;
+    k = (int)(m - 1);
+    const long long j = ((long long)k * n1 + B - 1) / B;
+    next = (int)(j * B / n1); err = (int)(j * B % n1);
+  }
+  __device__ __forceinline__ void advance() {
+    if (whole) { ++k; return; }
+    if (first) { k = hop(k); return; }
+    for (++k; k == next; ++k) next = hop(next);
+  }
+  __device__ __forceinline__ int hop(int p) {
+    p += step;
+    if ((err += rem) >= own) { err -= own; ++p; }
+    return p;
+  }
 };
 
 __device__ __forceinline__ void tma_load_raw(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -123,22 +180,22 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = s_tmem;
   chain_begin();
-  const long long u0 = start_of(g, (int)blockIdx.x);
-  const int run = (int)(start_of(g, (int)blockIdx.x + 1) - u0);
-  Walk at(g, u0);
+  const int cta = (int)blockIdx.x;
+  Walk at(g, cta);
 
   if (warp == kTmaWarp) {
     if (elect_one()) {
       bool ok = true;
       int n = 0;
-      for (; n < run; ++n, at.next(g)) {
+      Order order(g, at, cta);
+      int tl, ts;
+      tile_of(g, at.tile, &tl, &ts);
+      for (; at.len > 0; ++n) {
         // the long side's ring is free again when a block has been split, the short side's when the products have read it
         const uint32_t s = (uint32_t)(n % kStages), parity = ((uint32_t)(n / kStages) & 1u) ^ 1u, to = ring + s * kLongBytes;
         ok = !s_abort && mbar_wait(empty + 8 * s, parity, limit) && !g.stall;
         if (!ok) break;
-        int tl, ts;
-        tile_of(g, at.tile, &tl, &ts);
-        const int k0 = at.block * kBlockK, l0 = tl * kRows;
+        const int k0 = order.k * kBlockK, l0 = tl * kRows;
         mbar_expect(full + 8 * s, (uint32_t)kLongBytes);
         if (g.l_rows_inner) {
           tma_load_raw(to, &map_l, l0, k0, full + 8 * s);
@@ -151,6 +208,12 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
         mbar_expect(sfull + 8 * s, (uint32_t)Z::kShortBytes);
 #pragma unroll
         for (int p = 0; p < 3; ++p) tma_load<1>(shorts + s * Z::kShortBytes + p * kBN * 128, &map_s, k0, ts * kBN, p, sfull + 8 * s);
+        order.advance();
+        if (++at.at == at.len) {
+          at.next_piece(g, cta);
+          order = Order(g, at, cta);
+          tile_of(g, at.tile, &tl, &ts);
+        }
       }
       if (!ok) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
       // every stage filled is used up before the shared memory goes; having given up, what is under way gets its time to land
@@ -164,6 +227,7 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
     }
     __syncwarp();
   } else if (warp >= kEpiWarps && warp < kEpiWarps + kSplitWarps) {
+    const int run = g.rounds * g.blocks + (cta < g.shared ? g.own : g.shared > 0 ? (int)(at.end - helper_start(g, cta - g.shared)) : 0);
     // two groups of four warps, a block each in turn, so that the latencies of one overlap the other's work; a lane per row
     const int row = (warp & 3) * 32 + lane, group = (warp - kEpiWarps) >> 2;
     bool ok = true;
@@ -222,13 +286,14 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
       constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24);      // bfloat16, k along memory in B
       bool ok = true;
       uint32_t v = 0;
-      for (int n = 0; n < run && ok; ++v) {
-        // a segment: up to kSegment blocks of one tile
-        const int len = min(min(kSegment, run - n), g.blocks - at.block);
+      int n = 0;
+      while (ok && at.len > 0) {
+        // a segment: up to kSegment blocks of one piece
+        const int len = min(kSegment, at.len - at.at);
         ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(tempty + 8 * (v & 1u), ((v >> 1) & 1u) ^ 1u, limit));
         if (!ok) break;
         const uint32_t d = tmem + (v & 1u) * Z::kD;
-        for (int i = 0; i < len; ++i, ++n, at.next(g)) {
+        for (int i = 0; i < len; ++i, ++n) {
           const uint32_t s = (uint32_t)(n % kStages), b = (uint32_t)(n % Z::kSets);
           ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(sfull + 8 * s, (uint32_t)(n / kStages) & 1u, limit) &&
                                        mbar_wait(afull + 8 * b, (uint32_t)(n / Z::kSets) & 1u, limit));
@@ -251,6 +316,8 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
         if (!ok) break;
         if (one) umma_commit<1>(tfull + 8 * (v & 1u));
         __syncwarp();
+        ++v;
+        if ((at.at += len) == at.len) at.next_piece(g, cta);
       }
       if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     }
@@ -258,13 +325,11 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   } else {
     bool ok = true;
     uint32_t v = 0;
-    for (int n = 0; n < run && ok;) {
-      // a piece: this CTA's blocks of one tile
-      const int piece = min(run - n, g.blocks - at.block);
+    for (; ok && at.len > 0; at.next_piece(g, cta)) {
       float acc[kBN];
 #pragma unroll
       for (int j = 0; j < kBN; ++j) acc[j] = 0.f;
-      for (int k = 0; k < piece && ok; k += kSegment, ++v) {
+      for (int k = 0; k < at.len && ok; k += kSegment, ++v) {
         ok = !s_abort && mbar_wait(tfull + 8 * (v & 1u), (v >> 1) & 1u, limit);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
@@ -289,7 +354,7 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
       tile_of(g, at.tile, &tl, &ts);
       const int row = warp * 32 + lane;
       const long long l = (long long)tl * kRows + row;
-      if (piece == g.blocks) {
+      if (at.slot < 0) {
 #pragma unroll
         for (int c = 0; c < kBN; c += 16) {
           float z[16];
@@ -298,14 +363,11 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
           if (ts * kBN + c < g.ns) finish_split<16>(g, z, l, ts * kBN + c);
         }
       } else {
-        float* p = g.partial + ((long long)(2 * blockIdx.x + (n == 0 ? 0 : 1)) * kBN) * kRows + row;
+        float* p = g.partial + (long long)at.slot * kBN * kRows + row;
 #pragma unroll
         for (int j = 0; j < kBN; ++j) p[j * kRows] = acc[j];
       }
       __syncwarp();
-      n += piece;
-      at.block += piece;
-      if (at.block == g.blocks) { at.block = 0; ++at.tile; }
     }
     if (!ok && lane == 0) { s_abort = 1; atomicOr(g.status, STRADS_STATUS_WAIT_EXPIRED); }
     __syncwarp();
@@ -319,34 +381,36 @@ k_linear_split(const __grid_constant__ CUtensorMap map_l, const __grid_constant_
   }
 }
 
-// Tiles that fell to more than one CTA, eight columns to a CTA, adding in the order of the CTAs.
+// The shared tiles, eight columns to a CTA: the first CTA's sums, and the helpers' in their order.
 template <int kBN>
 __global__ void __launch_bounds__(256) k_linear_split_sum(const __grid_constant__ SplitArgs g) {
   chain_begin();
   __shared__ int s_first, s_last;
-  __shared__ bool s_begins;                              // the first of the tile's CTAs begins with it (else with the tile before)
+  __shared__ bool s_any[kMostCtas];                      // (with few blocks left to share, some helpers have none)
   const int t = blockIdx.x;
   if (threadIdx.x == 0) {
-    const long long b0 = (long long)t * g.blocks, b1 = b0 + g.blocks;
-    // the CTA that holds the tile's first block: near b0 ctas / (all blocks)
-    int c = (int)(b0 * g.ctas / ((long long)g.tiles_l * g.tiles_s * g.blocks));
-    while (c + 1 < g.ctas && start_of(g, c + 1) <= b0) ++c;
-    while (c > 0 && start_of(g, c) > b0) --c;
-    s_first = c;
-    s_begins = start_of(g, c) == b0;
-    while (c + 1 < g.ctas && start_of(g, c + 1) < b1) ++c;
-    s_last = c;
+    const long long left = g.blocks - g.own, b0 = t * left, b1 = b0 + left;
+    // the helper that holds what is left of the tile first: near b0 helpers / (all that is left)
+    int h = (int)(b0 * (g.ctas - g.shared) / (left * g.shared));
+    while (helper_start(g, h + 1) <= b0) ++h;
+    while (h > 0 && helper_start(g, h) > b0) --h;
+    s_first = h;
+    while (helper_start(g, h + 1) < b1) ++h;
+    s_last = h;
   }
+  for (int h = threadIdx.x; h < g.ctas - g.shared; h += 256) s_any[h] = helper_start(g, h) < helper_start(g, h + 1);
   __syncthreads();
-  const int c0 = s_first, c1 = s_last;
-  if (c0 == c1) return;                                  // one CTA had all of it and has finished it
   int tl, ts;
-  tile_of(g, t, &tl, &ts);
+  tile_of(g, g.rounds * g.ctas + t, &tl, &ts);
   const int row = threadIdx.x & (kRows - 1), col = blockIdx.y * 8 + (threadIdx.x >> 7) * 4;
   if (ts * kBN + col >= g.ns) return;
-  float v[4] = {};
-  for (int c = c0; c <= c1; ++c) {
-    const float* p = g.partial + ((long long)(2 * c + (c > c0 || s_begins ? 0 : 1)) * kBN + col) * kRows + row;
+  float v[4];
+  const float* p = g.partial + ((long long)t * kBN + col) * kRows + row;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = p[j * kRows];
+  for (int h = s_first; h <= s_last; ++h) {
+    if (!s_any[h]) continue;
+    p = g.partial + ((long long)(g.shared + t + h) * kBN + col) * kRows + row;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] += p[j * kRows];
   }
@@ -381,7 +445,7 @@ cudaError_t launch(const Operand& L, const Planes& S, long long nk, const SplitA
   if (!encode_long(&ml, L, g.nl, nk) || !encode_operand(&ms, S, true, kBN)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(k_linear_split<kBN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sizes<kBN>::kSmem);
   if (e == cudaSuccess) e = launch_chained(k_linear_split<kBN>, dim3((unsigned)g.ctas), kThreads, Sizes<kBN>::kSmem, s, ml, ms, g);
-  if (e == cudaSuccess && g.ctas > 1) e = launch_chained(k_linear_split_sum<kBN>, dim3((unsigned)(g.tiles_l * g.tiles_s), kBN / 8), 256, 0, s, g);
+  if (e == cudaSuccess && g.shared > 0 && g.own < g.blocks) e = launch_chained(k_linear_split_sum<kBN>, dim3((unsigned)g.shared, kBN / 8), 256, 0, s, g);
   return e;
 }
 
@@ -394,7 +458,7 @@ bool linear_split_takes(const Operand& L, long long nl, long long nk) {
 }
 
 size_t linear_split_workspace(long long nl, long long ns, long long nk) {
-  return (size_t)2 * ctas_of(nl, ns, nk) * width_of(ns) * kRows * sizeof(float);
+  return (size_t)2 * ctas_of(nl, ns, nk) * width_of(ns) * kRows * sizeof(float);      // (R < ctas)
 }
 
 cudaError_t launch_linear_split(const Operand& L, const Planes& S, long long nl, long long ns, long long nk, bool long_is_b, const Finish& f,
@@ -405,6 +469,10 @@ cudaError_t launch_linear_split(const Operand& L, const Planes& S, long long nl,
   g.tiles_l = (int)((nl + kRows - 1) / kRows);
   g.tiles_s = (int)((ns + width_of(ns) - 1) / width_of(ns));
   g.ctas = ctas_of(nl, ns, nk);
+  const long long tiles = (long long)g.tiles_l * g.tiles_s;
+  g.rounds = (int)(tiles / g.ctas);
+  g.shared = (int)(tiles % g.ctas);
+  g.own = (int)(((long long)g.shared * g.blocks + g.ctas - 1) / g.ctas);
   g.l_rows_inner = L.ks != 1;
   g.long_is_b = long_is_b; g.stall = stall;
   g.partial = static_cast<float*>(workspace);

@@ -224,6 +224,22 @@ def test_what_is_not_finite_stays_in_its_row(b, dtype, n):
         assert torch.isfinite(gx[others]).all() and not torch.isfinite(gb).any()
 
 
+@pytest.mark.parametrize("tiles,blocks", [(1, 1), (1, 3), (1, 40), (2, 9), (5, 31), (147, 2), (148, 3), (149, 3), (150, 2), (300, 2), (37, 16)])
+@pytest.mark.parametrize("order", ["rows", "cols"])
+def test_shares_of_tiles(b, tiles, blocks, order):
+    """binary32 with few rows on one side: tiles of 128 rows by blocks of 64 k, however they divide among the CTAs; NaN in the memory that
+    the partial sums get."""
+    n, k = 128 * tiles - 5, 64 * blocks - 3
+    gen = torch.Generator(device="cuda").manual_seed(tiles)
+    whole = torch.full((k, n + 5) if order == "cols" else (n, k + 3), float("nan"), device="cuda")      # runs that start on 16 bytes, NaN behind them
+    x = whole[:, :n].t() if order == "cols" else whole[:, :k]
+    x.copy_(torch.randn(n, k, generator=gen, device="cuda"))
+    for m in (7, 33, 50):
+        junk = torch.full((64 << 20,), float("nan"), device="cuda")
+        del junk
+        check_forward(b, x, matrix(m, k, torch.float32, gen, scale=k ** -0.5), None, None, "identity", 1.0)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_no_rows(b, dtype):
     x, w = torch.empty(0, 30, dtype=dtype, device="cuda"), torch.randn(20, 30, device="cuda").to(dtype)
