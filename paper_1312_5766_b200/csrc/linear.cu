@@ -186,6 +186,13 @@ bool vec_rows(const void* p, long long pitch, long long rows, size_t size) {
   return ((uintptr_t)p & 15) == 0 && (rows == 1 || (pitch * (long long)size) % 16 == 0);
 }
 
+// Whether TMA reads a 16-bit operand where it is: one of its strides 1, the other and its start on 16 bytes.
+bool in_place(const Operand& m, long long rows, long long nk) {
+  const bool rows_inner = m.ks != 1 && (m.rs == 1 || rows == 1) && nk > 1;
+  const long long inner = rows_inner ? rows : nk, outer = rows_inner ? nk : rows, outer_stride = rows_inner ? m.ks : m.rs, inner_stride = rows_inner ? m.rs : m.ks;
+  return (inner_stride == 1 || inner == 1) && ((uintptr_t)m.p & 15) == 0 && (outer == 1 || (outer_stride % 8 == 0 && outer_stride >= inner));
+}
+
 // `unknown`: where the matrix lies is not known yet (a workspace query), so that it has to be taken for one that is copied.
 Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unknown = false, bool k_inner = false) {
   const bool rows_inner = !k_inner && m.ks != 1 && (m.rs == 1 || rows == 1) && nk > 1;
@@ -195,7 +202,7 @@ Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unkno
   p.outer = rows_inner ? nk : rows;
   const long long outer_stride = rows_inner ? m.ks : m.rs, inner_stride = rows_inner ? m.rs : m.ks;
   p.planes = c.size == 4 ? 3 : 1;
-  if (!unknown && c.size == 2 && (inner_stride == 1 || p.inner == 1) && ((uintptr_t)m.p & 15) == 0 && (p.outer == 1 || (outer_stride % 8 == 0 && outer_stride >= p.inner))) {
+  if (!unknown && !k_inner && c.size == 2 && in_place(m, rows, nk)) {
     p.p = m.p;
     p.ld = p.outer == 1 ? (p.inner + 7) / 8 * 8 : outer_stride;
     return p;
@@ -258,14 +265,17 @@ Product plan(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
   d.b = tb ? Operand{B.m.p, B.m.ks, B.m.rs} : B.m;
   d.na = ta ? A.cols : A.rows; d.nb = tb ? B.cols : B.rows; d.nk = ta ? A.rows : A.cols;
   d.f = f;
-  d.way = Product::kThin;
-  if ((d.na < d.nb ? d.na : d.nb) <= kThinMost) return d;
-  // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 32 or 48
-  // rows, most of them from L2, where planes in memory cost 16)
   d.b_long = d.na < d.nb || (d.na == d.nb && B.order < A.order);
   const Operand &l = d.b_long ? d.b : d.a, &sh = d.b_long ? d.a : d.b;
   const long long nl = d.b_long ? d.nb : d.na, ns = d.b_long ? d.na : d.nb;
-  const bool unknown = (d.b_long ? B : A).unknown;       // (a query: room for either way)
+  const bool unknown = (d.b_long ? B : A).unknown;       // (a query: room for any way)
+  // Few rows on one side: streamed, if the tensor cores would first have to copy the long side or split it; 16-bit ones that they read where they are go
+  // there at once (4,096 x 4,096 bfloat16: 11 us whatever the rows, streamed 14 with two, 13 with four), but for one row with k along memory (10.7) and
+  // for long sides of so few rows that they make few tiles (64 rows of 16,384: 13.6, streamed 3.8).
+  d.way = Product::kThin;
+  if (ns <= kThinMost && !unknown && (c.size == 4 || !in_place(l, nl, d.nk) || (ns == 1 && l.ks == 1) || nl < 2048)) return d;
+  // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 32 or 48
+  // rows, most of them from L2, where planes in memory cost 16)
   if (c.size == 4 && ns <= kSplitMost && (unknown || linear_split_takes(l, nl, d.nk))) {
     d.way = Product::kSplit;
     d.pb = bring(c, sh, ns, d.nk, false, true);
