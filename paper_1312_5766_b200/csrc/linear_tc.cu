@@ -1,8 +1,8 @@
 // Products of linear layers on the 5th-generation tensor cores: D[a][b] = sum_k A[a][k] B[b][k], written through Finish.
 //
 // A tile of D is 128 kCG rows (a) by kBN columns (b).  One thread per CTA feeds a ring of stages with TMA tile loads (128-byte
-// swizzle, zero fill past the ends of a matrix), one issues tcgen05.mma kind::f16 into an FP32 accumulator in tensor memory, eight
-// warps read it back with tcgen05.ld and finish it, a lane per row: rows are side by side in D's memory, so every warp's
+// swizzle, zero fill past the ends of a matrix), one issues tcgen05.mma kind::f16 into an FP32 accumulator in tensor memory, eight or
+// sixteen warps read it back with tcgen05.ld and finish it, a lane per row: rows are side by side in D's memory, so every warp's
 // store is one run of it.  Either operand may have its rows or its k running through memory (the descriptors say which).
 // kCG = 2: two CTAs of a cluster share a tile of 256 rows, each holding its 128 rows of A and half of B, which halves what is
 // loaded per product; the first one issues the MMAs for both.
@@ -28,9 +28,6 @@ namespace {
 
 constexpr int kRows = 128;                 // rows of A that a CTA holds
 constexpr int kBlockK = 64;                // 16-bit elements of k per stage = one 128-byte swizzle row
-constexpr int kEpiWarps = 8;
-constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
-constexpr int kThreads = 32 * (kEpiWarps + 2);
 constexpr int kProducts = 6;               // of planes (binary32)
 constexpr uint32_t kWaitLimit = kMmaWaitLimit, kStallLimit = kMmaStallLimit;
 constexpr size_t kSmemMost = 227 * 1024;
@@ -42,13 +39,17 @@ struct Shape {
   static constexpr int kABytes = kRows * 128;
   static constexpr int kBBytes = (kCols < 64 ? 64 : kCols) * 128;          // (a box along the rows is at least 64 wide)
   static constexpr int kStageBytes = (kPlanes ? 3 : 1) * (kABytes + kBBytes);
-  static constexpr int kChunk = kPlanes || kBN < 128 ? 16 : 32;           // columns of the result that a warp finishes at a time
-  static constexpr int kSlotBytes = 2048;                                 // a chunk: 32 rows of them
+  // warps that finish results: sixteen hide the latencies of short tiles' epilogues (4,096 x 1,024 x 4,096 with everything in it: 47 us with eight)
+  static constexpr int kEpiWarps = kBN < 128 ? 8 : 16, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
+  static constexpr int kWarpCols = kBN / (kEpiWarps / 4);                 // columns of a tile that each of them reads back
+  static constexpr int kChunk = 16;                                       // columns of the result that a warp finishes at a time
+  static constexpr int kSlotBytes = kChunk * 32 * (int)sizeof(T);         // a chunk: 32 rows of them
   // narrow tiles read far more than they write: no shared memory for results, and two CTAs to an SM, so that up to 2 x 148 tiles
   // are under way at once and share the memory's bandwidth evenly however they divide by 148
   static constexpr bool kNarrow = kBN < 128;
-  // per warp two slots for what goes out and two for what comes in (binary32: the residual comes straight, 128 bytes an instruction)
-  static constexpr int kEpiBytes = kNarrow ? 0 : kEpiWarps * (kPlanes ? 2 : 4) * kSlotBytes;
+  // per warp two slots for what goes out and two for what comes in (binary32, whose stages need the room: one, and the residual comes straight, 128 bytes
+  // an instruction)
+  static constexpr int kEpiBytes = kNarrow ? 0 : kEpiWarps * (kPlanes ? 1 : 4) * kSlotBytes;
   static constexpr int kStages = (int)(((kNarrow && !kPlanes ? kSmemMost / 2 - 512 : kSmemMost) - 2048 - kEpiBytes) / kStageBytes);
   static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kEpiBytes + 1024;
   static constexpr uint32_t kTmemCols = 2 * kBN < 32 ? 32 : 2 * kBN;      // two accumulators
@@ -103,7 +104,7 @@ template <typename T, int kC>
 __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const CUtensorMap* map_out, const CUtensorMap* map_pre, float (&v)[kC],
                                              float bias, int a0, int b0, int lane, uint32_t limit) {
   const Finish& f = g.f;
-  constexpr int kRow = 32 * (int)sizeof(T);
+  constexpr int kRow = 32 * (int)sizeof(T), kSlot = kC * kRow, kOut = sizeof(T) == 4 ? 1 : 2;
   const long long a = a0 + lane;
   const bool here = a < g.na;
   const uint32_t mine = (uint32_t)lane * sizeof(T);
@@ -117,7 +118,7 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
       const uint32_t s = e.got & 1u;
       if (!__all_sync(0xffffffffu, mbar_wait(e.bar + 8 * s, (e.got >> 1) & 1u, limit))) return false;
 #pragma unroll
-      for (int j = 0; j < kC; ++j) r[j] = ld_shared(e.in + s * 2048 + j * kRow + mine, T());
+      for (int j = 0; j < kC; ++j) r[j] = ld_shared(e.in + s * kSlot + j * kRow + mine, T());
       ++e.got;
       __syncwarp();
     } else if (f.residual.p) {
@@ -133,8 +134,8 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
       for (int j = 0; j < kC; ++j) v[j] += load_f32(static_cast<const T*>(f.bias) + min(b0 + j, g.nb - 1));
     }
     if (g.preact_tma) {
-      const uint32_t slot = e.out + (e.put++ & 1u) * 2048;
-      if (lane == 0) tma_stores_read<1>();
+      const uint32_t slot = e.out + (e.put++ % kOut) * kSlot;
+      if (lane == 0) tma_stores_read<kOut - 1>();
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
@@ -159,8 +160,8 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
     for (int j = 0; j < kC; ++j) v[j] *= f.scale;
   }
   if (g.out_tma) {
-    const uint32_t slot = e.out + (e.put++ & 1u) * 2048;
-    if (lane == 0) tma_stores_read<1>();
+    const uint32_t slot = e.out + (e.put++ % kOut) * kSlot;
+    if (lane == 0) tma_stores_read<kOut - 1>();
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
@@ -176,12 +177,12 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
 }
 
 template <typename T, int kBN, int kCG>
-__global__ void __launch_bounds__(kThreads, kBN < 128 && sizeof(T) == 2 ? 2 : 1)
+__global__ void __launch_bounds__(Shape<T, kBN, kCG>::kThreads, kBN < 128 && sizeof(T) == 2 ? 2 : 1)
 k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
             const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ TcArgs g) {
   using S = Shape<T, kBN, kCG>;
   constexpr bool kPlanes = S::kPlanes;
-  constexpr int kHalf = kBN / 2;                         // columns of a tile that an epilogue warp reads back
+  constexpr int kEpiWarps = S::kEpiWarps, kTmaWarp = S::kTmaWarp, kMmaWarp = S::kMmaWarp, kCols = S::kWarpCols;
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_tfull[2], s_tempty[2], s_in[kEpiWarps][2];
   __shared__ uint32_t s_tmem;
@@ -319,19 +320,19 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
     __syncwarp();
   } else {
-    const int quarter = warp & 3, half = warp >> 2;      // tensor memory lanes 32 quarter .. , columns half * kHalf ..
+    const int quarter = warp & 3, part = warp >> 2;      // tensor memory lanes 32 quarter .. , columns part * kCols ..
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    constexpr int kC = S::kChunk, kChunks = kHalf / kC;
+    constexpr int kC = S::kChunk, kChunks = kCols / kC;
     uint32_t u = 0;
     bool ok = true;
     Epilogue e;
-    e.out = tiles + S::kStages * S::kStageBytes + warp * (kPlanes ? 2 : 4) * S::kSlotBytes;
+    e.out = tiles + S::kStages * S::kStageBytes + warp * (kPlanes ? 1 : 4) * S::kSlotBytes;
     e.in = e.out + 2 * S::kSlotBytes;
     e.bar = smem_u32(s_in) + 16 * warp;
     e.asked = e.got = e.put = 0;
     for (int i = first; i < n_items && ok; i += stride) {
       const Item w = item_of(g, i, split);
-      const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + half * kHalf;
+      const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + part * kCols;
       const int seg = kPlanes ? 1 : w.blocks;
       // chunks that lie in D at all
       const int chunks = a0 < g.na && b0 < g.nb ? min(kChunks, (g.nb - b0 + kC - 1) / kC) : 0;
@@ -340,7 +341,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (g.splits == 1 && g.residual_tma && c < chunks) {
           if (lane == 0) {
             mbar_expect(e.bar + 8 * (e.asked & 1u), 32 * kC * (uint32_t)sizeof(T));
-            tma_load_2d(e.in + (e.asked & 1u) * 2048, &map_res, a0, b0 + c * kC, e.bar + 8 * (e.asked & 1u));
+            tma_load_2d(e.in + (e.asked & 1u) * S::kSlotBytes, &map_res, a0, b0 + c * kC, e.bar + 8 * (e.asked & 1u));
           }
           ++e.asked;
         }
@@ -348,19 +349,19 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       ask(0);
       float bias = 0.f;
       if (g.f.bias && g.f.bias_b == 0 && a0 + lane < g.na) bias = load_f32(static_cast<const T*>(g.f.bias) + (a0 + lane));
-      float acc[kPlanes ? kHalf : kC];
+      float acc[kPlanes ? kCols : kC];
       if (kPlanes)
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) acc[j] = 0.f;
+        for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
       for (int k = 0; k < w.blocks && ok; k += seg, ++u) {
         ok = !s_abort && mbar_wait(tfull + 8 * (u & 1u), (u >> 1) & 1u, limit);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + (u & 1u) * kBN + lanes + half * kHalf;
+        const uint32_t d = tmem + (u & 1u) * kBN + lanes + part * kCols;
         if (kPlanes) {
 #pragma unroll
-          for (int c = 0; c < kHalf / 16; ++c) {
+          for (int c = 0; c < kCols / 16; ++c) {
             uint32_t v[16];
             tmem_load16(d + c * 16, v);
             tmem_wait();
@@ -386,7 +387,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             } else {
 #pragma unroll
               for (int j = 0; j < kC; ++j)               // (the ring is drained: all of it has been read by the MMAs)
-                st_shared(tiles + (uint32_t)(((half * kHalf + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
+                st_shared(tiles + (uint32_t)(((part * kCols + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
             }
           }
         }
@@ -407,7 +408,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
           } else {
 #pragma unroll
             for (int j = 0; j < kC; ++j)
-              st_shared(tiles + (uint32_t)(((half * kHalf + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
+              st_shared(tiles + (uint32_t)(((part * kCols + c * kC + j) * kRows + quarter * 32 + lane) * 4), x[j]);
           }
         }
       }
@@ -429,9 +430,10 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       const int row = threadIdx.x & (kRows - 1);
       const long long a = (long long)w.ta * kRows + row;
       // a thread's columns: col, col + step, .., several at a time
-      constexpr int kN = S::kNarrow ? 4 : 8;
-      const int step = 2 * g.splits, end = min(kBN, g.nb - w.tb * kBN);
-      for (int col = split * 2 + (int)(threadIdx.x >> 7); col < end; col += kN * step) {
+      constexpr int kN = 4;
+      constexpr int kGroups = kEpiWarps / 4;
+      const int step = kGroups * g.splits, end = min(kBN, g.nb - w.tb * kBN);
+      for (int col = split * kGroups + (int)(threadIdx.x >> 7); col < end; col += kN * step) {
         const int count = min(kN, (end - col + step - 1) / step);
         float z[kN];
 #pragma unroll
@@ -479,12 +481,12 @@ cudaError_t allow_all() {
   return e;
 }
 template <typename K>
-int clusters_that_fit(K kernel, int size, size_t smem) {
+int clusters_that_fit(K kernel, int size, int threads, size_t smem) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)size; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)size * 64); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = dim3((unsigned)size * 64); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem;
   cfg.attrs = attr; cfg.numAttrs = 1;
   int n = 0;
   const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
@@ -503,9 +505,9 @@ cudaError_t device_of(const Device** out) {
     if (tensor_map_encoder() == nullptr) return cudaErrorNotSupported;
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
     if ((e = allow_all<float>()) != cudaSuccess || (e = allow_all<__nv_bfloat16>()) != cudaSuccess || (e = allow_all<__half>()) != cudaSuccess) return e;
-    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<__nv_bfloat16, 256, 2>::kSmem);
+    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<__nv_bfloat16, 256, 2>::kThreads, Shape<__nv_bfloat16, 256, 2>::kSmem);
     if (d.pairs < 1) return cudaErrorNotSupported;
-    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<__nv_bfloat16, 128, 1>::kSmem);
+    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<__nv_bfloat16, 128, 1>::kThreads, Shape<__nv_bfloat16, 128, 1>::kSmem);
     d.known = true;
   }
   *out = &d;
@@ -535,7 +537,7 @@ cudaError_t launch(const Planes& A, const Planes& B, TcArgs g, unsigned ctas, cu
     g.residual_tma = !S::kPlanes && encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
     g.preact_tma = encode_result<T>(&mp, g.f.preact, g.na, g.nb, kC);
   }
-  return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
+  return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, S::kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
