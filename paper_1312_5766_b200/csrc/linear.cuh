@@ -31,10 +31,12 @@ __device__ __forceinline__ void store_f32(__half* p, float v) { *p = __float2hal
 // For binary32 results (kExact) CUDA's exponential and quotient, for 16-bit ones the hardware's, good to 2^-20.  Phi(-z), z >= 0, is exp(-z^2/2)
 // t P(t), t = 1 / (1 + 0.285 z): P is fitted to erfcx, weighted so that the relative error is even (1.6e-7; 4.7e-7 as evaluated here).  Nothing
 // cancels for negative z in any of them.
+__device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float fast_exp(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f)); return r; }
 template <bool kExact>
-__device__ __forceinline__ float sigmoid_f32(float z) { return kExact ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float sigmoid_f32(float z) { return kExact ? 1.f / (1.f + expf(-z)) : fast_inverse(1.f + fast_exp(-z)); }
 __device__ __forceinline__ float normal_tail(float a, float e) {      // Phi(-a), e = exp(-a^2/2)
-  const float t = __fdividef(1.f, fmaf(0.285f, a, 1.f));
+  const float t = fast_inverse(fmaf(0.285f, a, 1.f));
   float p = 0.024569256f;
   p = fmaf(p, t, -0.08659119f);
   p = fmaf(p, t, 0.07391585f);
@@ -54,7 +56,7 @@ __device__ __forceinline__ float activate_as(float z) {
   if (kAct == STRADS_ACT_RELU) return z < 0.f ? 0.f : z;               // (a NaN stays one)
   if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z);
   if (kAct == STRADS_ACT_GELU) {
-    const float q = z * normal_tail(fabsf(z), kExact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z));
+    const float q = z * normal_tail(fabsf(z), kExact ? expf(-0.5f * z * z) : fast_exp(-0.5f * z * z));
     return z > 0.f ? z - q : q;
   }
   if (kAct == STRADS_ACT_GELU_TANH) return z * sigmoid_f32<kExact>(tanh_argument2(z));
@@ -66,7 +68,7 @@ __device__ __forceinline__ float slope_as(float z) {
   if (kAct == STRADS_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
   if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z) * sigmoid_f32<kExact>(-z);
   if (kAct == STRADS_ACT_GELU) {
-    const float e = kExact ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
+    const float e = kExact ? expf(-0.5f * z * z) : fast_exp(-0.5f * z * z);
     const float near = fminf(fmaxf(z, -40.f), 40.f);                   // (beyond, e is 0)
     const float q = normal_tail(fabsf(z), e);
     return fmaf(near * 0.3989422804014327f, e, z > 0.f ? 1.f - q : q);

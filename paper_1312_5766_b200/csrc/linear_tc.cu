@@ -94,6 +94,7 @@ template <typename T> __device__ __forceinline__ T as_type(float v) { T t; store
 struct Epilogue {
   uint32_t in, out, bar;                 // shared memory: two slots each; the two barriers of what comes in
   uint32_t asked, got, put;              // chunks of the residual asked for and used; slots stored from
+  bool one;                              // the lane that issues the copies
 };
 
 // A chunk of kC columns (b0 ..) of 32 rows (a0 ..; this lane: a0 + lane).  Through shared memory a column is one run of 32 rows,
@@ -135,13 +136,13 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
     }
     if (g.preact_tma) {
       const uint32_t slot = e.out + (e.put++ % kOut) * kSlot;
-      if (lane == 0) tma_stores_read<kOut - 1>();
+      if (e.one) tma_stores_read<kOut - 1>();
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) tma_store_2d(map_pre, slot, a0, b0);
+      if (e.one) tma_store_2d(map_pre, slot, a0, b0);
     } else if (f.preact.p && here) {
 #pragma unroll
       for (int j = 0; j < kC; ++j)
@@ -161,13 +162,13 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
   }
   if (g.out_tma) {
     const uint32_t slot = e.out + (e.put++ % kOut) * kSlot;
-    if (lane == 0) tma_stores_read<kOut - 1>();
+    if (e.one) tma_stores_read<kOut - 1>();
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < kC; ++j) st_shared(slot + j * kRow + mine, as_type<T>(v[j]));
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (lane == 0) tma_store_2d(map_out, slot, a0, b0);
+    if (e.one) tma_store_2d(map_out, slot, a0, b0);
   } else if (here) {
 #pragma unroll
     for (int j = 0; j < kC; ++j)
@@ -330,6 +331,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     e.in = e.out + 2 * S::kSlotBytes;
     e.bar = smem_u32(s_in) + 16 * warp;
     e.asked = e.got = e.put = 0;
+    e.one = elect_one();
     for (int i = first; i < n_items && ok; i += stride) {
       const Item w = item_of(g, i, split);
       const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + part * kCols;
@@ -339,7 +341,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       // the residual's next chunk is asked for a chunk ahead, a tile's first while its sums are still being formed
       auto ask = [&](int c) {
         if (g.splits == 1 && g.residual_tma && c < chunks) {
-          if (lane == 0) {
+          if (e.one) {
             mbar_expect(e.bar + 8 * (e.asked & 1u), 32 * kC * (uint32_t)sizeof(T));
             tma_load_2d(e.in + (e.asked & 1u) * S::kSlotBytes, &map_res, a0, b0 + c * kC, e.bar + 8 * (e.asked & 1u));
           }
@@ -413,7 +415,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
       }
     }
-    if (lane == 0) {                                     // nothing of this warp's is under way when the shared memory goes
+    if (e.one) {                                         // nothing of this warp's is under way when the shared memory goes
       for (; e.got != e.asked; ++e.got)
         if (!mbar_wait(e.bar + 8 * (e.got & 1u), (e.got >> 1) & 1u, limit)) break;
       asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
