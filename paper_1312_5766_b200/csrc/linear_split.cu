@@ -13,7 +13,7 @@
 // Every CTA has the same number of blocks, however the tiles divide.  With W CTAs, each first takes whole tiles, the CTAs' tiles side by side; of the R
 // tiles left, CTAs 0 .. R - 1 take n1 = R B / W of the B blocks of one each, spread evenly over k, and the other W - R what is left of them.  So at any
 // time the CTAs read the same few k of neighbouring rows: runs of blocks of one tile after another, each CTA at a k of its own, read a column-major design
-// at 5.1 TB/s, where tiles in step reach 6.5.  The tiles shared are left as partial sums in the workspace and finished by a second kernel, in a
+// at 5.1 TB/s, where tiles in step reach 5.6.  The tiles shared are left as partial sums in the workspace and finished by a second kernel, in a
 // fixed order.  Waits are bounded as in linear_tc.cu.
 #include "linear_tc.cuh"
 #include "linear_ptx.cuh"

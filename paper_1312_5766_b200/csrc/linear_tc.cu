@@ -39,10 +39,12 @@ struct Shape {
   static constexpr int kABytes = kRows * 128;
   static constexpr int kBBytes = (kCols < 64 ? 64 : kCols) * 128;          // (a box along the rows is at least 64 wide)
   static constexpr int kStageBytes = (kPlanes ? 3 : 1) * (kABytes + kBBytes);
-  // warps that finish results: sixteen hide the latencies of short tiles' epilogues (4,096 x 1,024 x 4,096 with everything in it: 47 us with eight)
-  static constexpr int kEpiWarps = kBN < 128 ? 8 : 16, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
+  // warps that finish results: sixteen where the epilogue is long for its products (binary32, 4,096^3 with GELU and residual: 815 -> 695 us) or a tile is
+  // small; eight, 32 columns at a time, for pairs' tiles of 16 bits, whose products sixteen slow down (8,192^3: 734 against 758 us, with everything in the
+  // epilogue 759 against 787; 4,096 x 1,024 x 4,096: 28.5 against 30.3, with everything 43.6 against 42.9)
+  static constexpr int kEpiWarps = kBN < 128 || (kBN == 256 && !kPlanes) ? 8 : 16, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
   static constexpr int kWarpCols = kBN / (kEpiWarps / 4);                 // columns of a tile that each of them reads back
-  static constexpr int kChunk = 16;                                       // columns of the result that a warp finishes at a time
+  static constexpr int kChunk = kBN >= 128 && kEpiWarps == 8 ? 32 : 16;   // columns of the result that a warp finishes at a time
   static constexpr int kSlotBytes = kChunk * 32 * (int)sizeof(T);         // a chunk: 32 rows of them
   // narrow tiles read far more than they write: no shared memory for results, and two CTAs to an SM, so that up to 2 x 148 tiles
   // are under way at once and share the memory's bandwidth evenly however they divide by 148
