@@ -35,6 +35,14 @@ __device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.appro
 __device__ __forceinline__ float fast_exp(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f)); return r; }
 template <bool kExact>
 __device__ __forceinline__ float sigmoid_f32(float z) { return kExact ? 1.f / (1.f + expf(-z)) : fast_inverse(1.f + fast_exp(-z)); }
+// sigma(z) and sigma(-z) by one exponential and one inverse: with e = exp(-|z|) they are 1 / (1 + e) and e / (1 + e) (gradient with SiLU, 4,096 x 8,192
+// bfloat16 by 64: 62.0 us, 66.2 with two of each).
+struct Sigmoids { float at, opposite; };
+template <bool kExact>
+__device__ __forceinline__ Sigmoids sigmoids_f32(float z) {
+  const float e = kExact ? expf(-fabsf(z)) : fast_exp(-fabsf(z)), near = kExact ? 1.f / (1.f + e) : fast_inverse(1.f + e), far = e * near;
+  return z < 0.f ? Sigmoids{far, near} : Sigmoids{near, far};
+}
 __device__ __forceinline__ float normal_tail(float a, float e) {      // Phi(-a), e = exp(-a^2/2)
   const float t = fast_inverse(fmaf(0.285f, a, 1.f));
   float p = 0.024569256f;
@@ -66,7 +74,10 @@ __device__ __forceinline__ float activate_as(float z) {
 template <bool kExact, int kAct>
 __device__ __forceinline__ float slope_as(float z) {
   if (kAct == STRADS_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-  if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z) * sigmoid_f32<kExact>(-z);
+  if (kAct == STRADS_ACT_SIGMOID) {
+    const Sigmoids s = sigmoids_f32<kExact>(z);
+    return s.at * s.opposite;
+  }
   if (kAct == STRADS_ACT_GELU) {
     const float e = kExact ? expf(-0.5f * z * z) : fast_exp(-0.5f * z * z);
     const float near = fminf(fmaxf(z, -40.f), 40.f);                   // (beyond, e is 0)
@@ -75,10 +86,13 @@ __device__ __forceinline__ float slope_as(float z) {
   }
   if (kAct == STRADS_ACT_GELU_TANH) {
     const float u = tanh_argument2(z), near = fminf(fmaxf(z, -40.f), 40.f);      // (beyond, the second term is 0)
-    const float s = sigmoid_f32<kExact>(u), o = sigmoid_f32<kExact>(-u);
-    return fmaf(near * s * o, 1.5957691216057308f * fmaf(0.134145f * near, near, 1.f), s);
+    const Sigmoids s = sigmoids_f32<kExact>(u);
+    return fmaf(near * s.at * s.opposite, 1.5957691216057308f * fmaf(0.134145f * near, near, 1.f), s.at);
   }
-  if (kAct == STRADS_ACT_SILU) return sigmoid_f32<kExact>(z) * fmaf(z, sigmoid_f32<kExact>(-z), 1.f);
+  if (kAct == STRADS_ACT_SILU) {
+    const Sigmoids s = sigmoids_f32<kExact>(z);
+    return s.at * fmaf(z, s.opposite, 1.f);
+  }
   return 1.f;
 }
 
