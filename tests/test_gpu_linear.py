@@ -409,3 +409,61 @@ def test_the_binding_refuses(b):
                  lambda: b.linear_forward(x, w, out=torch.zeros(1, 3, device="cuda").expand(4, 3))):
         with pytest.raises(b.StradsError):
             call()
+
+
+# results of 74 tiles of 256 x 256 and more, which pairs of CTAs form: last tiles of 1, 8, 10, 36 and 255 rows or columns, results that TMA can address and
+# (2,570) cannot, one block of k and several
+PAIRS = [(2305, 70, 2568), (2340, 1, 2570), (2340, 200, 2568), (2559, 130, 2312), (4097, 64, 1288)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("i", range(len(PAIRS)), ids=lambda i: "x".join(map(str, PAIRS[i])))
+def test_tiles_of_pairs(b, i, dtype):
+    n, k, m = PAIRS[i]
+    for turn, act in enumerate(ACTS):
+        gen = torch.Generator(device="cuda").manual_seed(1000 + 10 * i + turn)
+        x = matrix(n, k, dtype, gen, "rows" if turn % 2 == 0 else "cols")
+        w = matrix(m, k, dtype, gen, "cols" if turn % 3 == 0 else "rows", scale=k ** -0.5)
+        bias = torch.randn(m, generator=gen, device="cuda").to(dtype) if turn % 3 else None
+        residual = matrix(n, m, dtype, gen, "cols" if turn == 4 else "rows") if turn != 1 else None
+        out = matrix(n, m, dtype, gen, "cols" if turn in (2, 4) else "rows", pad=(0, 8)[turn == 5])
+        check_forward(b, x, w, bias, residual, act, (1.0, -1.0, 0.5)[turn % 3], out=out)
+        edge = out.as_strided((n, 8), (m + 8, 1), out.storage_offset() + m) if turn == 5 else None
+        assert edge is None or torch.isnan(edge).all()   # what lies between the rows stays
+        # the same tiles as a gradient: gx is n x m
+        gout, v = matrix(n, k, dtype, gen), matrix(k, m, dtype, gen, "cols" if turn % 2 else "rows", scale=k ** -0.5)
+        z = matrix(n, k, dtype, gen) if act != "identity" else None
+        check_backward(b, gout, matrix(n, m, dtype, gen), v, z, act, 0.5)
+
+
+def test_threads_on_streams_of_their_own(b):
+    """Four threads at once, each with a stream, calls and workspaces of its own: the bits of the same calls one after another."""
+    import threading
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    cases = [(1000, 500, 20, torch.float32), (24, 900, 700, torch.bfloat16), (2340, 100, 2568, torch.float16), (333, 1001, 517, torch.float32)]
+    inputs = [(matrix(n, k, t, gen), matrix(m, k, t, gen, scale=0.05), matrix(n, m, t, gen)) for n, k, m, t in cases]
+
+    def once(x, w, g):
+        out, z = b.linear_forward(x, w, activation="silu", want_preact=True)
+        return [out, *b.linear_backward(g, x, w, preact=z, activation="silu")]
+
+    want = [once(*v) for v in inputs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got = once(*inputs[i])
+                    if not all(torch.equal(p, q) for p, q in zip(got, want[i])):
+                        wrong.append(i)
+        except Exception as e:
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and b.linear_status() == (0, 0)
