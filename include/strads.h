@@ -316,14 +316,15 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  *   residual = y and scale = -1 it is the paper's residual y - X beta for each of them (Section 2.1), and with the sigmoid
  *   y - sigma(X beta), the logistic loss's.
  * strads_linear_backward:  from gout = dF/dout and the z kept by the forward pass (not read with the identity)
- *   gz = scale gout act'(z),   gx = gz w,   gw = gz^T x,   gbias = column sums of gz     (each only where asked for)
+ *   gz = gout act'(z),   gx = scale gz w,   gw = scale gz^T x,   gbias = scale times the column sums of gz     (each only where asked for)
  *   dF/dresidual is gout itself.  act'(0) of the ReLU is 0.  n_rows = 0: gw and gbias are noughts.
  *
  * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more.  binary32 products go through three
  * bfloat16 parts of each operand (24 bits together) on the tensor cores, or are formed as they are where one side has few
- * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: gz is rounded to the type where the products
- * read it (as a framework that keeps it would), an error as large as the result's own rounding: gx and gw through an activation
- * are about sqrt(2) further from the formula than with gz in 32 bits; gbias is not.  z is rounded once, behind act.
+ * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: gz (without scale) is rounded to the type where the
+ * products read it (as a framework that keeps it would), an error as large as the result's own rounding where gz is a normal number of its
+ * type: gx and gw through an activation are about sqrt(2) further from the formula than with gz in 32 bits; gbias is not.
+ * z is rounded once, behind act.
  * GELU is z Phi(z), GELU_TANH its tanh form 1/2 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), SILU z sigma(z).
  *
  * Matrices may have any strides (elements; >= 0 for what is read, so rows and columns may be repeated with stride 0; what is

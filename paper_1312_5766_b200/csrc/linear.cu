@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_pack(const __grid_constant_
   }
 }
 
-// ---- gz = scale gout act'(preact), and its column sums ----
+// ---- gz = gout act'(preact), and its column sums ----
+// (scale stays outside, a factor of the 32-bit sums as it is with the identity: inside, gz of binary16 would leave its range with it.)
 // A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row, kU of them at a time so that their loads are under way
 // together.  Three CTAs to an SM (80 registers): the pass waits for memory, and warps hide that better than rows of one lane (gradient of 4,096 x 8,192
 // bfloat16 by 64, SiLU / GELU: 62 / 69 us; four rows at a time and one CTA 99 / 80, two CTAs 66 / 75; four CTAs 60 / 66, with spills that cost binary32
@@ -81,7 +82,7 @@ __device__ __forceinline__ void load8(const T* p, long long stride, int count, T
   }
 }
 template <typename T, int kAct, bool kVec>
-__device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, float scale, T* gz, long long ld, long long c, long long r0,
+__device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, T* gz, long long ld, long long c, long long r0,
                                         long long r1, int warp, float (&total)[8]) {
   constexpr int kU = 2;
   const int count = (int)min(8ll, m - c);
@@ -99,7 +100,7 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
       __align__(16) T out[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float v = scale * load_f32(&g[u][j]);
+        float v = load_f32(&g[u][j]);
         if (kAct != STRADS_ACT_IDENTITY) v *= slope_as<sizeof(T) == 4, kAct>(load_f32(&z[u][j]));
         if (kVec || j < count) total[j] += v;
         store_f32(&out[j], v);
@@ -111,15 +112,15 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
   }
 }
 template <typename T, int kAct>
-__global__ void __launch_bounds__(kThreads, 3) k_linear_gz(Operand gout, Operand preact, long long n, long long m, float scale, T* gz, long long ld,
+__global__ void __launch_bounds__(kThreads, 3) k_linear_gz(Operand gout, Operand preact, long long n, long long m, T* gz, long long ld,
                                                         float* partial, long long rows, int vec) {
   __shared__ float sum[8][256 + 8];
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
   float total[8] = {};
-  if (vec && c + 8 <= m) gz_rows<T, kAct, true>(gout, preact, m, scale, gz, ld, c, r0, r1, warp, total);
-  else if (c < m) gz_rows<T, kAct, false>(gout, preact, m, scale, gz, ld, c, r0, r1, warp, total);
+  if (vec && c + 8 <= m) gz_rows<T, kAct, true>(gout, preact, m, gz, ld, c, r0, r1, warp, total);
+  else if (c < m) gz_rows<T, kAct, false>(gout, preact, m, gz, ld, c, r0, r1, warp, total);
   if (partial == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[warp][j * 33 + lane] = total[j];
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_linear_gz(Operand gout, Operand
 }
 // 32 columns to a CTA, eight warps taking a run of the blocks of rows each.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_linear_bias_grad(const float* partial, int blocks, long long m, T* gbias) {
+__global__ void __launch_bounds__(kThreads) k_linear_bias_grad(const float* partial, int blocks, long long m, float scale, T* gbias) {
   __shared__ float sum[8][32];
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_bias_grad(const float* part
   if (warp == 0 && c < m) {
 #pragma unroll
     for (int w = 1; w < 8; ++w) s += sum[w][lane];
-    store_f32(gbias + c, s);
+    store_f32(gbias + c, scale * s);
   }
 }
 
@@ -338,7 +339,7 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
   if (preact) z = operand_of(*preact);
   const int vec = gout.col_stride == 1 && vec_rows(gout.data, gout.row_stride, g.n_rows, sizeof(T)) &&
                   (g.activation == STRADS_ACT_IDENTITY || (z.ks == 1 && vec_rows(z.p, z.rs, g.n_rows, sizeof(T))));
-  void (*kernel)(Operand, Operand, long long, long long, float, T*, long long, float*, long long, int) = k_linear_gz<T, STRADS_ACT_IDENTITY>;
+  void (*kernel)(Operand, Operand, long long, long long, T*, long long, float*, long long, int) = k_linear_gz<T, STRADS_ACT_IDENTITY>;
   switch (g.activation) {
     case STRADS_ACT_RELU: kernel = k_linear_gz<T, STRADS_ACT_RELU>; break;
     case STRADS_ACT_SIGMOID: kernel = k_linear_gz<T, STRADS_ACT_SIGMOID>; break;
@@ -348,9 +349,9 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
     default: break;
   }
   c.err = launch_chained(kernel, dim3((unsigned)columns, (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
-                         g.scale, gz, ld, partial, rows, vec);
+                         gz, ld, partial, rows, vec);
   if (gbias != nullptr && c.err == cudaSuccess)
-    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, gbias);
+    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, g.scale, gbias);
 }
 
 template <typename T>
@@ -364,7 +365,7 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
       c.err = launch_chained(k_linear_zero<T>, ctas_for(g.n_out), kThreads, 0, c.stream, static_cast<T*>(gbias), 1ll, (long long)g.n_out, (long long)g.n_out, 1ll);
     return;
   }
-  // the identity's gz is gout itself, its scale a factor of the results; otherwise gz is formed, and its column sums on the way
+  // the identity's gz is gout itself; otherwise gz is formed, and its column sums on the way; scale is a factor of the results
   const bool formed = g.activation != STRADS_ACT_IDENTITY;
   const long long ld = (g.n_out + 7) / 8 * 8;
   T* gz = formed ? static_cast<T*>(c.take((size_t)g.n_rows * (size_t)ld * sizeof(T))) : nullptr;
@@ -375,7 +376,7 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
   z.unknown = !formed && c.all;
   Finish f = {};
   f.plain = 1;
-  f.scale = formed ? 1.f : g.scale;
+  f.scale = g.scale;
   Product dx = {}, dw = {};
   if (gx != nullptr || c.all) {
     const bool ar = gx != nullptr && rows_run(gx->row_stride, gx->col_stride);
