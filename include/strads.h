@@ -321,9 +321,10 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  *
  * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more.  binary32 products go through three
  * bfloat16 parts of each operand (24 bits together) on the tensor cores, or are formed as they are where one side has few
- * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: gz (without scale) is rounded to the type where the
- * products read it (as a framework that keeps it would), an error as large as the result's own rounding where gz is a normal number of its
- * type: gx and gw through an activation are about sqrt(2) further from the formula than with gz in 32 bits; gbias is not.
+ * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: through an activation gz (without scale) is rounded
+ * where the products read it, an error as large as the result's own rounding: gx and gw are about sqrt(2) further from the formula than with gz in
+ * 32 bits; gbias is not.  bfloat16's gz is rounded to the type; binary16's to its 11 bits with a power of two of its row (for gx) or column (for gw), so
+ * that it neither overflows nor vanishes: what is below 2^-29 of the largest finite |gout| of that row or column is off by up to 2^-39 of that.
  * z is rounded once, behind act.
  * GELU is z Phi(z), GELU_TANH its tanh form 1/2 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), SILU z sigma(z).
  *

@@ -11,6 +11,44 @@ __device__ unsigned int g_linear_status;       // STRADS_STATUS_* bits of the la
 
 constexpr int kThreads = 256;
 
+// ---- lines of binary16 gradients (see k_linear_tops) ----
+// 2^-e for the power 2^e that brings a magnitude to 2^14 .. 2^15, and 2^e from that.  (A line of noughts: 2^126.)
+__device__ __forceinline__ float line_factor(unsigned int half_bits) {
+  const unsigned int b = __float_as_uint(__half2float(__ushort_as_half((unsigned short)half_bits)));
+  return __uint_as_float((max(b >> 23, 15u) - 14u) << 23);
+}
+__device__ __forceinline__ float line_power(float factor) { return __uint_as_float((254u << 23) - __float_as_uint(factor)); }
+// The largest magnitudes of the blocks of rows (columns: [blocks][m]) and of the blocks of 256 columns (rows: [columns][n]), and the factors to be formed from them:
+// those of columns by the first `column_ctas` CTAs, 32 each, of rows by the others, 256 each.
+struct LinesJob {
+  const unsigned short *col_tops, *row_tops;
+  float *column_factors, *row_factors;
+  long long n, m;
+  int blocks, columns, column_ctas, ctas;
+};
+__device__ __forceinline__ void form_factors(const LinesJob& j, int cta, unsigned int (&top)[8][32]) {
+  unsigned int t = 0u;
+  if (cta >= j.column_ctas) {
+    const long long r = (long long)(cta - j.column_ctas) * kThreads + threadIdx.x;
+    if (r >= j.n) return;
+#pragma unroll 4
+    for (int i = 0; i < j.columns; ++i) t = max(t, (unsigned int)j.row_tops[i * j.n + r]);
+    j.row_factors[r] = line_factor(t);
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)cta * 32 + lane;
+  if (c < j.m)
+#pragma unroll 4
+    for (int r = j.blocks * warp / 8; r < j.blocks * (warp + 1) / 8; ++r) t = max(t, (unsigned int)j.col_tops[r * j.m + c]);
+  top[warp][lane] = t;
+  __syncthreads();
+  if (warp != 0 || c >= j.m) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) t = max(t, top[w][lane]);
+  j.column_factors[c] = line_factor(t);
+}
+
 // ---- operands of the tensor-core products that cannot be read in place ----
 // dst[plane][outer][ld] from src, eight neighbours per thread; binary32 as three planes of bfloat16 (split_pair).  All operands of a call that
 // need it in one launch.
@@ -21,7 +59,7 @@ struct Copy {
   int vec;
 };
 constexpr int kMostCopies = 3;
-struct Copies { Copy c[kMostCopies]; int n; long long groups; };
+struct Copies { Copy c[kMostCopies]; int n, ctas; long long groups; };      // (the first `ctas` CTAs of the launch)
 template <typename T>
 __device__ __forceinline__ void copy_group(const Copy& c, long long i) {
   const long long per = c.ld / 8, o = i / per, k = i % per * 8;
@@ -53,10 +91,15 @@ __device__ __forceinline__ void copy_group(const Copy& c, long long i) {
   }
 }
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_linear_pack(const __grid_constant__ Copies all) {
+__global__ void __launch_bounds__(kThreads) k_linear_pack(const __grid_constant__ Copies all, const __grid_constant__ LinesJob lines) {
+  __shared__ unsigned int top[8][32];
   chain_begin();
+  if ((int)blockIdx.x >= all.ctas) {
+    form_factors(lines, (int)blockIdx.x - all.ctas, top);
+    return;
+  }
   // the groups of all matrices as one run, so that a thread's loads do not wait for those of another matrix
-  const long long stride = (long long)gridDim.x * kThreads;
+  const long long stride = (long long)all.ctas * kThreads;
   for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all.groups; i += stride) {
     long long at = i;
     int n = 0;
@@ -67,6 +110,63 @@ __global__ void __launch_bounds__(kThreads) k_linear_pack(const __grid_constant_
 
 // ---- gz = gout act'(preact), and its column sums ----
 // (scale stays outside, a factor of the 32-bit sums as it is with the identity: inside, gz of binary16 would leave its range with it.)
+// binary16, through an activation: gz may lie above 65,504, or below 2^-14 where the type has fewer digits or none, although the sums over it are numbers of the
+// type.  It is held with a power of two that brings the largest finite |gout| of a line to 2^14 .. 2^15 (and so gz below 1.13 times that): of its row in the copy that
+// gx is formed from, of its column in gw's; the products' epilogue takes the power back.  What is below 2^-29 of that |gout| is off by up to 2^-39 of it.
+// k_linear_tops looks at gout alone: half of what forms gz, and no exponentials (SiLU, all launches of a gradient of 4,096 x 8,192 by 64: 119 us, from gz itself 156, with
+// gz rounded as it is 80; 2,048^3: 73, 78, 63; 333 x 1,001 x 517: 31, 31, 26).
+struct Lines { const float *row_factors, *column_factors; __half* by_column; };      // 2^-e of every row and column; gz with its column's power (gz: with its row's)
+constexpr unsigned int kHalfAbs = 0x7fff7fffu, kHalfInfinity = 0x7c007c00u;
+__device__ __forceinline__ unsigned int finite_halves(unsigned int x) {      // magnitudes of two of them, 0 for what is not finite
+  x &= kHalfAbs;
+  return x & ~__vcmpgeu2(x, kHalfInfinity);
+}
+// col_tops [gridDim.y][m] of the CTA's rows, row_tops [gridDim.x][n] of its 256 columns (each may be null), as bits of the type.
+__global__ void __launch_bounds__(kThreads) k_linear_tops(Operand gout, long long n, long long m, unsigned short* col_tops, unsigned short* row_tops, long long rows, int vec) {
+  constexpr int kU = 4;
+  __shared__ uint4 top[8][32];
+  chain_begin();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
+  const int count = (int)min(8ll, m - c);
+  const bool whole = vec && count == 8;
+  uint4 most = {0u, 0u, 0u, 0u};
+  for (long long r = r0 + warp; r < r1; r += 8 * kU) {
+    uint4 x[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      x[u] = {0u, 0u, 0u, 0u};
+      const unsigned short* p = static_cast<const unsigned short*>(gout.p) + min(r + 8 * u, r1 - 1) * gout.rs + c * gout.ks;
+      if (whole) {
+        x[u] = __ldg(reinterpret_cast<const uint4*>(p));
+      } else if (count > 0) {                            // (past the last column: that column again)
+        unsigned int w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = p[min(j, count - 1) * gout.ks];
+        x[u] = {w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16};
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      x[u] = {finite_halves(x[u].x), finite_halves(x[u].y), finite_halves(x[u].z), finite_halves(x[u].w)};
+      most = {__vmaxu2(most.x, x[u].x), __vmaxu2(most.y, x[u].y), __vmaxu2(most.z, x[u].z), __vmaxu2(most.w, x[u].w)};
+      if (row_tops != nullptr) {
+        const unsigned int t = __vmaxu2(__vmaxu2(x[u].x, x[u].y), __vmaxu2(x[u].z, x[u].w)), all = __reduce_max_sync(0xffffffffu, max(t >> 16, t & 0xffffu));
+        if (lane == 0 && r + 8 * u < r1) row_tops[(long long)blockIdx.x * n + r + 8 * u] = (unsigned short)all;
+      }
+    }
+  }
+  if (col_tops == nullptr) return;
+  top[warp][lane] = most;
+  __syncthreads();
+  const long long col = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (col >= m) return;
+  unsigned int t = 0u;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) t = max(t, (unsigned int)reinterpret_cast<const unsigned short*>(&top[w][0])[threadIdx.x]);
+  col_tops[(long long)blockIdx.y * m + col] = (unsigned short)t;
+}
+
 // A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row, kU of them at a time so that their loads are under way
 // together.  Three CTAs to an SM (80 registers): the pass waits for memory, and warps hide that better than rows of one lane (gradient of 4,096 x 8,192
 // bfloat16 by 64, SiLU / GELU: 62 / 69 us; four rows at a time and one CTA 99 / 80, two CTAs 66 / 75; four CTAs 60 / 66, with spills that cost binary32
@@ -83,9 +183,14 @@ __device__ __forceinline__ void load8(const T* p, long long stride, int count, T
 }
 template <typename T, int kAct, bool kVec>
 __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& preact, long long m, T* gz, long long ld, long long c, long long r0,
-                                        long long r1, int warp, float (&total)[8]) {
+                                        long long r1, int warp, const Lines& lines, float (&total)[8]) {
+  constexpr bool kLines = std::is_same<T, __half>::value && kAct != STRADS_ACT_IDENTITY;
   constexpr int kU = 2;
   const int count = (int)min(8ll, m - c);
+  float power[kLines ? 8 : 1];
+  if (kLines && lines.by_column != nullptr)
+#pragma unroll
+    for (int j = 0; j < (kLines ? 8 : 0); ++j) power[j] = line_power(lines.column_factors[c + min(j, count - 1)]);
   for (long long r = r0 + warp; r < r1; r += 8 * kU) {
     __align__(16) T g[kU][8], z[kU][8];
 #pragma unroll
@@ -98,13 +203,17 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
     for (int u = 0; u < kU; ++u) {
       if (r + 8 * u >= r1) break;
       __align__(16) T out[8];
+      __align__(16) T out_c[kLines ? 8 : 1];
+      const float row_power = kLines && gz != nullptr ? line_power(lines.row_factors[r + 8 * u]) : 1.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float v = load_f32(&g[u][j]);
         if (kAct != STRADS_ACT_IDENTITY) v *= slope_as<sizeof(T) == 4, kAct>(load_f32(&z[u][j]));
         if (kVec || j < count) total[j] += v;
-        store_f32(&out[j], v);
+        store_f32(&out[j], kLines ? v * row_power : v);
+        if (kLines) store_f32(&out_c[kLines ? j : 0], v * power[kLines ? j : 0]);
       }
+      if (kLines && lines.by_column != nullptr) *reinterpret_cast<uint4*>(lines.by_column + (r + 8 * u) * ld + c) = *reinterpret_cast<const uint4*>(out_c);
       if (gz != nullptr)                                 // (ld is a multiple of 8: the last group has its place)
 #pragma unroll
         for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(gz + (r + 8 * u) * ld + c)[j] = reinterpret_cast<const uint4*>(out)[j];
@@ -113,14 +222,14 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
 }
 template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 3) k_linear_gz(Operand gout, Operand preact, long long n, long long m, T* gz, long long ld,
-                                                        float* partial, long long rows, int vec) {
+                                                        float* partial, long long rows, int vec, Lines lines) {
   __shared__ float sum[8][256 + 8];
   chain_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long c = (long long)blockIdx.x * 256 + lane * 8, r0 = (long long)blockIdx.y * rows, r1 = min(n, r0 + rows);
   float total[8] = {};
-  if (vec && c + 8 <= m) gz_rows<T, kAct, true>(gout, preact, m, gz, ld, c, r0, r1, warp, total);
-  else if (c < m) gz_rows<T, kAct, false>(gout, preact, m, gz, ld, c, r0, r1, warp, total);
+  if (vec && c + 8 <= m) gz_rows<T, kAct, true>(gout, preact, m, gz, ld, c, r0, r1, warp, lines, total);
+  else if (c < m) gz_rows<T, kAct, false>(gout, preact, m, gz, ld, c, r0, r1, warp, lines, total);
   if (partial == nullptr) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[warp][j * 33 + lane] = total[j];
@@ -173,6 +282,7 @@ struct Call {
   cudaError_t err;
   unsigned int* status;
   Copies copies;                         // to be made before the next product
+  LinesJob lines;                        // likewise, in the same launch
   void* take(size_t bytes) {
     void* p = ws + used;
     used += (bytes + 255) / 256 * 256;
@@ -220,15 +330,17 @@ Planes bring(Call& c, const Operand& m, long long rows, long long nk, bool unkno
                               inner_stride == 1 && vec_rows(m.p, outer_stride, p.outer, c.size)};
   return p;
 }
-// The copies asked for so far, in one launch.
+// The copies asked for so far, and the factors of lines, in one launch.
 void copy(Call& c) {
-  if (!c.run || c.err != cudaSuccess || c.copies.n == 0) return;
+  if (!c.run || c.err != cudaSuccess || (c.copies.n == 0 && c.lines.ctas == 0)) return;
   c.copies.groups = 0;
   for (int i = 0; i < c.copies.n; ++i) c.copies.groups += c.copies.c[i].plane / 8;
-  const unsigned grid = ctas_for(c.copies.groups);
-  c.err = c.size == 4 ? launch_chained(k_linear_pack<float>, grid, kThreads, 0, c.stream, c.copies)
-                      : launch_chained(k_linear_pack<__half>, grid, kThreads, 0, c.stream, c.copies);
+  c.copies.ctas = c.copies.n > 0 ? (int)ctas_for(c.copies.groups) : 0;
+  const unsigned grid = (unsigned)(c.copies.ctas + c.lines.ctas);
+  c.err = c.size == 4 ? launch_chained(k_linear_pack<float>, grid, kThreads, 0, c.stream, c.copies, c.lines)
+                      : launch_chained(k_linear_pack<__half>, grid, kThreads, 0, c.stream, c.copies, c.lines);
   c.copies.n = 0;
+  c.lines.ctas = 0;
 }
 
 // A matrix as one side of products, brought into the workspace at most once: the other side of its transpose is the same copy.
@@ -323,23 +435,66 @@ void forward(Call& c, const strads_linear_config_t& g, const void* bias, const s
   launch(c, d);
 }
 
+// gz = gout act'(z) and its column sums: the places of what they need, and their kernels' arguments.  The products read gz from `for_x` and `for_w`; binary16's, through an
+// activation, with the factors of the lines that their results keep.
 template <typename T>
-void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, T* gz, long long ld, T* gbias) {
+struct Gz {
+  bool formed, by_lines;
+  long long columns, rows, ld;           // blocks of 256 columns, and of `rows` rows
+  int blocks;
+  T *for_x, *for_w;
+  unsigned short *row_tops, *col_tops;
+  float *row_factors, *column_factors, *partial;
+};
+template <typename T>
+Gz<T> plan_z(Call& c, const strads_linear_config_t& g, bool want_x, bool want_w, bool want_bias) {
+  Gz<T> k = {};
+  k.formed = g.activation != STRADS_ACT_IDENTITY && (want_x || want_w);
+  k.by_lines = k.formed && std::is_same<T, __half>::value;
   // at most 128 blocks of rows; of 64 rows where that leaves four CTAs to an SM, else of as few as 8
-  const long long columns = (g.n_out + 255) / 256;
-  long long rows = (g.n_rows * columns + 4 * 148 - 1) / (4 * 148);
-  if (rows > 64) rows = 64;
-  if (rows * 128 < g.n_rows) rows = (g.n_rows + 127) / 128;
-  rows = (rows + 7) / 8 * 8;
-  const int blocks = (int)((g.n_rows + rows - 1) / rows);
-  float* partial = gbias != nullptr || c.all ? static_cast<float*>(c.take((size_t)blocks * (size_t)g.n_out * sizeof(float))) : nullptr;
+  k.columns = (g.n_out + 255) / 256;
+  k.rows = (g.n_rows * k.columns + 4 * 148 - 1) / (4 * 148);
+  if (k.rows > 64) k.rows = 64;
+  if (k.rows * 128 < g.n_rows) k.rows = (g.n_rows + 127) / 128;
+  k.rows = (k.rows + 7) / 8 * 8;
+  k.blocks = (int)((g.n_rows + k.rows - 1) / k.rows);
+  k.ld = (g.n_out + 7) / 8 * 8;
+  const size_t n = (size_t)g.n_rows, m = (size_t)g.n_out, bytes = n * (size_t)k.ld * sizeof(T);
+  if (k.formed && (want_x || !k.by_lines)) k.for_x = static_cast<T*>(c.take(bytes));
+  k.for_w = k.by_lines && want_w ? static_cast<T*>(c.take(bytes)) : k.for_x;
+  if (k.by_lines && want_x) {
+    k.row_tops = static_cast<unsigned short*>(c.take(n * (size_t)k.columns * 2));
+    k.row_factors = static_cast<float*>(c.take(n * 4));
+  }
+  if (k.by_lines && want_w) {
+    k.col_tops = static_cast<unsigned short*>(c.take(m * (size_t)k.blocks * 2));
+    k.column_factors = static_cast<float*>(c.take(m * 4));
+  }
+  if (want_bias) k.partial = static_cast<float*>(c.take((size_t)k.blocks * m * sizeof(float)));
+  return k;
+}
+// What the factors of lines are formed from; they themselves come with the next copies.
+template <typename T>
+void tops_of_gout(Call& c, const Gz<T>& k, const strads_linear_config_t& g, const strads_const_matrix_t& gout) {
   if (!c.run || c.err != cudaSuccess) return;
+  const Operand o = operand_of(gout);
+  const long long n = g.n_rows, m = g.n_out;
+  const int vec = o.ks == 1 && vec_rows(o.p, o.rs, n, sizeof(T));
+  c.err = launch_chained(k_linear_tops, dim3((unsigned)k.columns, (unsigned)k.blocks), kThreads, 0, c.stream, o, n, m, k.col_tops, k.row_tops, k.rows, vec);
+  const int column_ctas = k.col_tops ? (int)((m + 31) / 32) : 0, row_ctas = k.row_tops ? (int)((n + kThreads - 1) / kThreads) : 0;
+  c.lines = {k.col_tops, k.row_tops, k.column_factors, k.row_factors, n, m, k.blocks, (int)k.columns, column_ctas, column_ctas + row_ctas};
+}
+template <typename T>
+void gradient_of_z(Call& c, const Gz<T>& k, const strads_linear_config_t& g, const strads_const_matrix_t& gout, const strads_const_matrix_t* preact, T* gbias) {
+  if (!c.run || c.err != cudaSuccess || (!k.formed && gbias == nullptr)) return;
   const Operand o = operand_of(gout);
   Operand z = {};
   if (preact) z = operand_of(*preact);
   const int vec = gout.col_stride == 1 && vec_rows(gout.data, gout.row_stride, g.n_rows, sizeof(T)) &&
                   (g.activation == STRADS_ACT_IDENTITY || (z.ks == 1 && vec_rows(z.p, z.rs, g.n_rows, sizeof(T))));
-  void (*kernel)(Operand, Operand, long long, long long, T*, long long, float*, long long, int) = k_linear_gz<T, STRADS_ACT_IDENTITY>;
+  Lines lines = {};
+  if constexpr (std::is_same<T, __half>::value) lines = {k.row_factors, k.column_factors, k.by_lines ? k.for_w : nullptr};
+  void (*kernel)(Operand, Operand, long long, long long, T*, long long, float*, long long, int, Lines) = k_linear_gz<T, STRADS_ACT_IDENTITY>;
   switch (g.activation) {
     case STRADS_ACT_RELU: kernel = k_linear_gz<T, STRADS_ACT_RELU>; break;
     case STRADS_ACT_SIGMOID: kernel = k_linear_gz<T, STRADS_ACT_SIGMOID>; break;
@@ -348,10 +503,10 @@ void gradient_of_z(Call& c, const strads_linear_config_t& g, const strads_const_
     case STRADS_ACT_SILU: kernel = k_linear_gz<T, STRADS_ACT_SILU>; break;
     default: break;
   }
-  c.err = launch_chained(kernel, dim3((unsigned)columns, (unsigned)blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
-                         gz, ld, partial, rows, vec);
+  c.err = launch_chained(kernel, dim3((unsigned)k.columns, (unsigned)k.blocks), kThreads, 0, c.stream, o, z, (long long)g.n_rows, (long long)g.n_out,
+                         k.for_x, k.ld, k.partial, k.rows, vec, lines);
   if (gbias != nullptr && c.err == cudaSuccess)
-    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(partial), blocks, (long long)g.n_out, g.scale, gbias);
+    c.err = launch_chained(k_linear_bias_grad<T>, dim3((unsigned)((g.n_out + 31) / 32)), kThreads, 0, c.stream, static_cast<const float*>(k.partial), k.blocks, (long long)g.n_out, g.scale, gbias);
 }
 
 template <typename T>
@@ -366,28 +521,35 @@ void backward(Call& c, const strads_linear_config_t& g, const strads_const_matri
     return;
   }
   // the identity's gz is gout itself; otherwise gz is formed, and its column sums on the way; scale is a factor of the results
-  const bool formed = g.activation != STRADS_ACT_IDENTITY;
-  const long long ld = (g.n_out + 7) / 8 * 8;
-  T* gz = formed ? static_cast<T*>(c.take((size_t)g.n_rows * (size_t)ld * sizeof(T))) : nullptr;
-  if (formed || gbias != nullptr || c.all) gradient_of_z<T>(c, g, gout, preact, gz, ld, static_cast<T*>(gbias));
-  Operand kept = operand_of(gout);
-  if (formed) { kept.p = gz; kept.rs = ld; kept.ks = 1; }
-  Matrix z = matrix_of(kept, g.n_rows, g.n_out, 2), x = matrix_of(operand_of(g.x), g.n_rows, g.n_in, 0), w = matrix_of(operand_of(g.w), g.n_out, g.n_in, 1);
-  z.unknown = !formed && c.all;
+  const bool want_x = gx != nullptr || c.all, want_w = gw != nullptr || c.all;
+  const Gz<T> gz = plan_z<T>(c, g, want_x, want_w, gbias != nullptr || c.all);
+  Operand for_x = operand_of(gout), for_w = for_x;
+  if (gz.formed) { for_x = {gz.for_x, gz.ld, 1}; for_w = {gz.for_w, gz.ld, 1}; }
+  Matrix z = matrix_of(for_x, g.n_rows, g.n_out, 2), z_w = matrix_of(for_w, g.n_rows, g.n_out, 2);
+  Matrix x = matrix_of(operand_of(g.x), g.n_rows, g.n_in, 0), w = matrix_of(operand_of(g.w), g.n_out, g.n_in, 1);
+  Matrix& zw = gz.by_lines ? z_w : z;      // (else one and the same, brought once)
+  z.unknown = !gz.formed && c.all;
   Finish f = {};
   f.plain = 1;
   f.scale = g.scale;
   Product dx = {}, dw = {};
-  if (gx != nullptr || c.all) {
+  if (want_x) {
     const bool ar = gx != nullptr && rows_run(gx->row_stride, gx->col_stride);
     if (gx != nullptr) f.out = side(gx->data, gx->row_stride, gx->col_stride, ar);
+    f.factor = gz.row_factors; f.factor_a = ar ? 1 : 0; f.factor_b = ar ? 0 : 1;
     dx = ar ? plan(c, z, false, w, true, f) : plan(c, w, true, z, false, f);
   }
-  if (gw != nullptr || c.all) {
+  if (want_w) {
     const bool ar = gw != nullptr && rows_run(gw->row_stride, gw->col_stride);
     if (gw != nullptr) f.out = side(gw->data, gw->row_stride, gw->col_stride, ar);
-    dw = ar ? plan(c, z, true, x, true, f) : plan(c, x, true, z, true, f);
+    f.factor = gz.column_factors; f.factor_a = ar ? 1 : 0; f.factor_b = ar ? 0 : 1;
+    dw = ar ? plan(c, zw, true, x, true, f) : plan(c, x, true, zw, true, f);
   }
+  if (gz.by_lines) {                     // (gz is read where it is: the copies are of others, and go with the factors that it needs)
+    tops_of_gout(c, gz, g, gout);
+    copy(c);
+  }
+  gradient_of_z(c, gz, g, gout, preact, static_cast<T*>(gbias));
   copy(c);
   launch(c, dx);
   launch(c, dw);

@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "strads_internal.cuh"
 
 namespace strads {
@@ -19,6 +21,8 @@ struct Finish {
   int act;
   float scale;
   int plain;                                                          // no bias, activation, residual, preact
+  const float* factor;                                                // plain results of binary16: element a factor_a + b factor_b; null = none
+  long long factor_a, factor_b;
 };
 
 __device__ __forceinline__ float load_f32(const float* p) { return *p; }
@@ -142,6 +146,11 @@ __device__ __forceinline__ void finish_run(const Finish& f, float (&v)[kN], long
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] = f.residual.p ? fmaf(f.scale, v[j], r[j]) : f.scale * v[j];
   } else {
+    if (std::is_same<T, __half>::value && f.factor) {
+      const float* p = f.factor + a * f.factor_a + b * f.factor_b;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] *= p[min(j, count - 1) * (step * f.factor_b)];
+    }
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] *= f.scale;
   }

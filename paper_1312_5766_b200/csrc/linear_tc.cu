@@ -158,9 +158,16 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
 #pragma unroll
       for (int j = 0; j < kC; ++j) v[j] *= f.scale;
     }
-  } else if (f.scale != 1.f) {
+  } else {
+    if (std::is_same<T, __half>::value && f.factor) {
+      const float* p = f.factor + (here ? a : g.na - 1) * f.factor_a;
 #pragma unroll
-    for (int j = 0; j < kC; ++j) v[j] *= f.scale;
+      for (int j = 0; j < kC; ++j) v[j] *= p[min(b0 + j, g.nb - 1) * f.factor_b];
+    }
+    if (f.scale != 1.f) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j) v[j] *= f.scale;
+    }
   }
   if (g.out_tma) {
     const uint32_t slot = e.out + (e.put++ % kOut) * kSlot;

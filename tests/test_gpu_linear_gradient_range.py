@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 
 def check_gradient(b, gout, x, w, z, act, scale, lost, slope_error=2.0 ** -20, relative=0.0):
-    """As check_backward of test_gpu_linear.py, with scale a factor of the sums.  lost(|gz|, dim): what an element of gz may lose beside eps / 2 of itself, where a
+    """As check_backward of test_gpu_linear.py, with scale a factor of the sums.  lost(|gout|, dim): what an element of gz may lose beside eps / 2 of itself, where a
     sum goes along dim.  slope_error: of the slope, as a part of the largest; relative: as a part of itself."""
     gx, gw, gb = b.linear_backward(gout, x, w, preact=z, activation=act, scale=scale)
     t = x.dtype
@@ -18,8 +18,8 @@ def check_gradient(b, gout, x, w, z, act, scale, lost, slope_error=2.0 ** -20, r
     own = gz.abs() * (2.0 ** -22 + relative) + slope_error * g.abs()
     e = own + u * gz.abs()
     (n, k), m = x.shape, w.shape[0]
-    for got, want, mag, err, terms in ((gx, gz @ w.to(F64), gz.abs() @ w.to(F64).abs(), (e + lost(gz.abs(), 1)) @ w.to(F64).abs(), m),
-                                       (gw, gz.t() @ x.to(F64), gz.abs().t() @ x.to(F64).abs(), (e + lost(gz.abs(), 0)).t() @ x.to(F64).abs(), n),
+    for got, want, mag, err, terms in ((gx, gz @ w.to(F64), gz.abs() @ w.to(F64).abs(), (e + lost(g.abs(), 1)) @ w.to(F64).abs(), m),
+                                       (gw, gz.t() @ x.to(F64), gz.abs().t() @ x.to(F64).abs(), (e + lost(g.abs(), 0)).t() @ x.to(F64).abs(), n),
                                        (gb, gz.sum(0), gz.abs().sum(0), own.sum(0), n)):
         want, tol = scale * want, s * ((terms + 16) * 2.0 ** -24 * mag + err)
         tol = tol + half_step(want.abs() + tol, t)
@@ -43,4 +43,72 @@ def test_scale_is_outside_of_the_rounding(b, act, size, scale, dtype):
         gout, z = matrix(n, m, dtype, gen, scale=size), matrix(n, m, dtype, gen)
         other = min(100.0, 100.0 / (size * scale) / max(m, n) ** 0.5)
         x, w = matrix(n, k, dtype, gen, scale=other), matrix(m, k, dtype, gen, "cols", scale=other)
-        check_gradient(b, gout, x, w, z, act, scale, lambda gz, dim: 2.0 ** -25 if dtype == torch.float16 else 0.0)
+        check_gradient(b, gout, x, w, z, act, scale, lambda g, dim: 2.0 ** -25 if dtype == torch.float16 else 0.0)
+
+
+def of_the_largest(g, dim):
+    """A power of two of the sum's own line brings its largest |gout| to 2^14 .. 2^15, so half a subnormal's step of gz, 2^-25, is at most 2^-39 of it."""
+    return 2.0 ** -39 * g.where(g.isfinite(), torch.zeros_like(g)).amax(dim, keepdim=True)
+
+
+@pytest.mark.parametrize("shape", [(8192, 24, 40), (40, 24, 8192), (8192, 3, 4), (4, 3, 8192), (1, 300, 8192), (8192, 300, 1), (1000, 129, 1001)])
+@pytest.mark.parametrize("outlier", [False, True])
+def test_gradients_below_the_types_range(b, shape, outlier):
+    """gout = 1e-4 by slopes of 1e-4, all of one sign: 1e-8, a third of what binary16 rounds to 0, adds up to what it does hold.  One row and one column of
+    gout at the other end of the range: the others keep what they had."""
+    n, k, m = shape
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    gout = (1e-4 * (1 + torch.rand(n, m, generator=gen, device="cuda"))).half()
+    if outlier:
+        gout[n // 2] = 3e4
+        gout[:, m // 2] = -2e4
+    z = (-9.2 - 0.3 * torch.rand(n, m, generator=gen, device="cuda")).half()
+    x, w = ((1 + torch.rand(*s, generator=gen, device="cuda")).half() for s in ((n, k), (m, k)))
+    # exp(-|z|): the product with log2 e is off by 2^-24 of 14, its power of two by 2^-22, inverse and products by 2^-22: below 2^-18 of the slope
+    check_gradient(b, gout, x, w, z, "sigmoid", 1.0, of_the_largest, slope_error=0.0, relative=2.0 ** -18)
+    if not outlier and 8192 in (n, m):
+        gx, gw, _ = b.linear_backward(gout, x, w, preact=z, activation="sigmoid")
+        assert ((gx if m == 8192 else gw) > 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_slopes_above_one_by_the_largest_numbers(b, act, dtype):
+    """gout at the type's largest number by slopes up to 1.13, x and w small enough for results inside the range (bfloat16, whose range is that of the sums: 2^118)."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n, k, m = 70, 40, 33
+    top = 65504.0 if dtype == torch.float16 else 2.0 ** 118
+    gout = torch.full((n, m), top, device="cuda").to(dtype)
+    z = (1.5 + torch.rand(n, m, generator=gen, device="cuda")).to(dtype)
+    x, w = matrix(n, k, dtype, gen, scale=0.01), matrix(m, k, dtype, gen, scale=0.01)
+    check_gradient(b, gout, x, w, z, act, 2.0 ** -8, of_the_largest)
+
+
+def test_rows_of_noughts_and_of_what_is_not_finite(b):
+    """A row without a gradient gives noughts; an infinity or NaN stays in its row of gx and its column's row of gw."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n, k, m = 130, 72, 90
+    gout, z, x, w = (matrix(*s, torch.float16, gen) for s in ((n, m), (n, m), (n, k), (m, k)))
+    gout[5] = 0
+    gout[:, 7] = 0
+    clean = b.linear_backward(gout, x, w, preact=z, activation="gelu")
+    assert not clean[0][5].any() and not clean[1][7].any() and not clean[2][7].any()
+    for value in (float("inf"), float("nan")):
+        bad = gout.clone()
+        bad[20, 30] = value
+        gx, gw, gb = b.linear_backward(bad, x, w, preact=z, activation="gelu")
+        rows, cols = [i for i in range(n) if i != 20], [i for i in range(m) if i != 30]
+        assert torch.equal(gx[rows], clean[0][rows]) and torch.equal(gw[cols], clean[1][cols]) and torch.equal(gb[cols], clean[2][cols])
+        assert not torch.isfinite(gx[20]).any() and not torch.isfinite(gw[30]).any() and not torch.isfinite(gb[30])
+
+
+@pytest.mark.parametrize("m", [7, 256, 257, 2000])
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 9000])
+def test_every_share_of_rows_and_columns(b, n, m):
+    """However rows and columns divide among CTAs: every row and column of a size of its own, between 2^-14 and 2^12."""
+    gen = torch.Generator(device="cuda").manual_seed(n + m)
+    k = 24
+    rows, cols = (torch.exp2(torch.randint(-7, 7, (c,), generator=gen, device="cuda").float()) for c in (n, m))
+    gout = (torch.randn(n, m, generator=gen, device="cuda") * rows[:, None] * cols).half()
+    z, x, w = (matrix(*s, torch.float16, gen, scale=f) for s, f in (((n, m), 1.0), ((n, k), 1e-3), ((m, k), 1e-3)))
+    check_gradient(b, gout, x, w, z, "silu", 0.5, of_the_largest)
