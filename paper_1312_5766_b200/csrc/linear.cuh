@@ -68,7 +68,8 @@ __device__ __forceinline__ float activate_as(float z) {
   if (kAct == STRADS_ACT_RELU) return z < 0.f ? 0.f : z;               // (a NaN stays one)
   if (kAct == STRADS_ACT_SIGMOID) return sigmoid_f32<kExact>(z);
   if (kAct == STRADS_ACT_GELU) {
-    const float q = z * normal_tail(fabsf(z), kExact ? expf(-0.5f * z * z) : fast_exp(-0.5f * z * z));
+    // (beyond 40 the tail is 0, and infinity times it would be NaN; -infinity times it is, as in the formula)
+    const float q = fminf(z, 40.f) * normal_tail(fabsf(z), kExact ? expf(-0.5f * z * z) : fast_exp(-0.5f * z * z));
     return z > 0.f ? z - q : q;
   }
   if (kAct == STRADS_ACT_GELU_TANH) return z * sigmoid_f32<kExact>(tanh_argument2(z));

@@ -1,0 +1,37 @@
+"""Activations and their slopes at infinities, NaN and the largest numbers of each type, through every kind of kernel."""
+import pytest
+import torch
+
+from test_gpu_linear import ACTS, F64, TYPES, act64, b  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def ends(dtype):
+    top = torch.finfo(dtype).max
+    return torch.tensor([float("inf"), float("-inf"), float("nan"), top, -top, 1e4, -1e4, 100.0, -100.0, 0.0, -0.0], dtype=dtype, device="cuda")
+
+
+def same(got, want, dtype):
+    """Equal where the value is 0 or not finite, NaN for NaN; else to the tolerance of a function and its rounding."""
+    got, want = got.double(), want.to(dtype).double()
+    assert torch.equal(got.isnan(), want.isnan())
+    keep = ~want.isnan()
+    got, want = got[keep], want[keep]
+    assert torch.equal(got.isinf(), want.isinf()) and torch.equal(got[want.isinf()], want[want.isinf()])
+    keep = want.isfinite()
+    # (binary32's sigma and Phi are 0 below 2^-126, and a number of 2^14 by them with it: 2^-112)
+    assert ((got[keep] - want[keep]).abs() <= (2.0 ** -19 + torch.finfo(dtype).eps) * want[keep].abs() + 2.0 ** -100).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n", [1, 3, 40, 300, 5000])
+def test_activations_at_the_ends(b, act, dtype, n):
+    """z = bias (x is 0) at both infinities, NaN and the largest numbers.  -inf by GELU, its tanh form and SiLU is -inf times 0: NaN, as in the formula."""
+    z = ends(dtype).repeat(n // 4 + 1)                   # (11 columns and up)
+    m = len(z)
+    for k in (8, 72):
+        out, keep = b.linear_forward(torch.zeros(n, k, dtype=dtype, device="cuda"), torch.ones(m, k, dtype=dtype, device="cuda"), bias=z, activation=act, want_preact=True)
+        same(keep, z.expand(n, m), dtype)
+        same(out, act64(z.to(F64), act).expand(n, m), dtype)
