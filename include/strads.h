@@ -327,7 +327,7 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  * that it neither overflows nor vanishes: what is below 2^-29 of the largest finite |gout| of that row or column is off by up to 2^-39 of that.
  * z is rounded once, behind act.
  * GELU is z Phi(z), GELU_TANH its tanh form 1/2 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), SILU z sigma(z); each is infinite at +infinity, and at
- * -infinity NaN, the formula's -infinity times 0.
+ * -infinity NaN, the formula's -infinity times 0.  Slopes at the infinities are their limits (a 16-bit z past the type's range is kept as one).
  *
  * Matrices may have any strides (elements; >= 0 for what is read, so rows and columns may be repeated with stride 0; what is
  * written must not overlap itself or any input, but out may be the residual itself).  Best are operands with one stride of 1,

@@ -96,7 +96,7 @@ __device__ __forceinline__ float slope_as(float z) {
   }
   if (kAct == STRADS_ACT_SILU) {
     const Sigmoids s = sigmoids_f32<kExact>(z);
-    return s.at * fmaf(z, s.opposite, 1.f);
+    return s.at * fmaf(fminf(fmaxf(z, -128.f), 128.f), s.opposite, 1.f);      // (beyond, one of the two is 0)
   }
   return 1.f;
 }

@@ -35,3 +35,26 @@ def test_activations_at_the_ends(b, act, dtype, n):
         out, keep = b.linear_forward(torch.zeros(n, k, dtype=dtype, device="cuda"), torch.ones(m, k, dtype=dtype, device="cuda"), bias=z, activation=act, want_preact=True)
         same(keep, z.expand(n, m), dtype)
         same(out, act64(z.to(F64), act).expand(n, m), dtype)
+
+
+LIMITS = {"relu": (1, 0), "sigmoid": (0, 0), "gelu": (1, 0), "gelu_tanh": (1, 0), "silu": (1, 0)}      # slopes far above and far below
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ACTS[1:])
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_slopes_at_the_ends(b, act, dtype, n):
+    """Far out the slope is its limit, at the infinities too (a z past the type's range is kept as one): one such z leaves the sums of its column finite."""
+    row = ends(dtype)[:9].repeat(4)
+    m = len(row)
+    above, below = LIMITS[act]
+    want = torch.where(row.isnan(), row.to(F64), torch.where(row > 0, above, below).to(F64)).expand(n, m)
+    z, one = row.expand(n, m), torch.ones(n, m, dtype=dtype, device="cuda")
+    gx, gw, gb = b.linear_backward(one, torch.ones(n, 16, dtype=dtype, device="cuda"), torch.eye(m, dtype=dtype, device="cuda")[:, :m][:, :16].contiguous(), preact=z, activation=act)
+    same(gb, want.sum(0), dtype)
+    same(gw, want.sum(0)[:, None].expand(m, 16), dtype)
+    if not want[:, :9].isnan().all():
+        # gx by the unit vectors: NaN columns make every sum NaN; without them the first 16 slopes are it
+        good = ~row.isnan()
+        gx, _, _ = b.linear_backward(one[:, good], torch.ones(n, 16, dtype=dtype, device="cuda"), torch.eye(int(good.sum()), 16, dtype=dtype, device="cuda"), preact=z[:, good], activation=act)
+        same(gx, want[:, good][:, :16], dtype)
