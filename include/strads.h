@@ -319,7 +319,8 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  *   gz = gout act'(z),   gx = scale gz w,   gw = scale gz^T x,   gbias = scale times the column sums of gz     (each only where asked for)
  *   dF/dresidual is gout itself.  act'(0) of the ReLU is 0.  n_rows = 0: gw and gbias are noughts.
  *
- * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more.  binary32 products go through three
+ * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more; where additions truncate (16-bit products), no more terms
+ * go into one accumulator than cost a tenth of the result's rounding.  binary32 products go through three
  * bfloat16 parts of each operand (24 bits together) on the tensor cores, or are formed as they are where one side has few
  * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: through an activation gz (without scale) is rounded
  * where the products read it, an error as large as the result's own rounding: gx and gw are about sqrt(2) further from the formula than with gz in

@@ -9,7 +9,7 @@
 //
 // binary32 operands come as three bfloat16 planes, x = p0 + p1 + p2 (24 bits).  A stage holds all of them for its 64 k, and of the nine products
 // of planes the six largest are formed, the smallest first.  The accumulator is emptied into registers after every block of k and added there with
-// rounding to nearest: the tensor cores' additions truncate (100,000 terms of one sign summed there: 2e-5 too small).
+// rounding to nearest: the tensor cores' additions truncate (emptied so, one-signed sums of 64 to 131,072 terms are 4.5e-8 too small, the worst of 60,000 4.2e-7).
 //
 // Few tiles: the CTAs of a cluster share a tile's k (splits > 1, kCG = 1), park their sums in shared memory and each finishes a share
 // of the columns, adding in the order of the CTAs.
@@ -32,9 +32,17 @@ constexpr int kProducts = 6;               // of planes (binary32)
 constexpr uint32_t kWaitLimit = kMmaWaitLimit, kStallLimit = kMmaStallLimit;
 constexpr size_t kSmemMost = 227 * 1024;
 
-template <typename T, int kBN, int kCG>
+// 16-bit operands with long k (kLong): the accumulator is emptied after runs of kRun blocks, and the runs are added in registers, as binary32's blocks are.
+constexpr int kRun = 64;
+// Blocks of k up to which one accumulator holds them all.  The tensor cores' additions truncate: a one-signed sum ends 6e-9 of itself too small for every term, so
+// that 8,192 (65,536) terms cost a tenth of the half step that binary16's (bfloat16's) result is rounded by.  Kept sums cost little: 2,309 x 2,310 by 16,384
+// binary16 175.7 us, with one accumulator 173.5; by 32,768 338 and 338; 40 x 100 by 131,072 81 and 80.
+constexpr int kMostHalf = 128, kMostBfloat = 1024;
+
+template <typename T, int kBN, int kCG, bool kLong>
 struct Shape {
-  static constexpr bool kPlanes = sizeof(T) == 4;
+  static constexpr bool kPlanes = sizeof(T) == 4, kKept = kPlanes || kLong;      // kKept: the sums of a tile are held in registers
+  static_assert(!(kPlanes && kLong), "binary32 empties the accumulator every block");
   static constexpr int kCols = kBN / kCG;                                  // rows of B that a CTA holds
   static constexpr int kABytes = kRows * 128;
   static constexpr int kBBytes = (kCols < 64 ? 64 : kCols) * 128;          // (a box along the rows is at least 64 wide)
@@ -44,7 +52,7 @@ struct Shape {
   // epilogue 759 against 787; 4,096 x 1,024 x 4,096: 28.5 against 30.3, with everything 43.6 against 42.9)
   static constexpr int kEpiWarps = kBN < 128 || (kBN == 256 && !kPlanes) ? 8 : 16, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
   static constexpr int kWarpCols = kBN / (kEpiWarps / 4);                 // columns of a tile that each of them reads back
-  static constexpr int kChunk = kBN >= 128 && kEpiWarps == 8 ? 32 : 16;   // columns of the result that a warp finishes at a time
+  static constexpr int kChunk = kBN >= 128 && kEpiWarps == 8 && !kLong ? 32 : 16;   // columns of the result that a warp finishes at a time
   static constexpr int kSlotBytes = kChunk * 32 * (int)sizeof(T);         // a chunk: 32 rows of them
   // narrow tiles read far more than they write: no shared memory for results, and two CTAs to an SM, so that up to 2 x 148 tiles
   // are under way at once and share the memory's bandwidth evenly however they divide by 148
@@ -186,12 +194,12 @@ __device__ __forceinline__ bool finish_chunk(const TcArgs& g, Epilogue& e, const
   return true;
 }
 
-template <typename T, int kBN, int kCG>
-__global__ void __launch_bounds__(Shape<T, kBN, kCG>::kThreads, kBN < 128 && sizeof(T) == 2 ? 2 : 1)
+template <typename T, int kBN, int kCG, bool kLong>
+__global__ void __launch_bounds__(Shape<T, kBN, kCG, kLong>::kThreads, kBN < 128 && sizeof(T) == 2 ? 2 : 1)
 k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
             const __grid_constant__ CUtensorMap map_res, const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ TcArgs g) {
-  using S = Shape<T, kBN, kCG>;
-  constexpr bool kPlanes = S::kPlanes;
+  using S = Shape<T, kBN, kCG, kLong>;
+  constexpr bool kPlanes = S::kPlanes, kKept = S::kKept;
   constexpr int kEpiWarps = S::kEpiWarps, kTmaWarp = S::kTmaWarp, kMmaWarp = S::kMmaWarp, kCols = S::kWarpCols;
   extern __shared__ unsigned char dyn[];
   __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_tfull[2], s_tempty[2], s_in[kEpiWarps][2];
@@ -296,13 +304,14 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       bool ok = true;
       for (int i = first; i < n_items && ok; i += stride) {
         const Item w = item_of(g, i, split);
-        const int seg = kPlanes ? 1 : w.blocks;          // blocks to an accumulator
+        const int seg = kPlanes ? 1 : kLong ? kRun : w.blocks;      // blocks to an accumulator
         for (int k = 0; k < w.blocks && ok; k += seg, ++u) {
           ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(tempty + 8 * (u & 1u), ((u >> 1) & 1u) ^ 1u, limit));
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t d = tmem + (u & 1u) * kBN;
-          for (int it = 0; it < seg; ++it, ++n) {
+          const int len = kLong ? min(seg, w.blocks - k) : seg;
+          for (int it = 0; it < len; ++it, ++n) {
             const uint32_t s = n % S::kStages;
             ok = __all_sync(0xffffffffu, !s_abort && mbar_wait(full + 8 * s, (n / S::kStages) & 1u, limit));
             if (!ok) break;
@@ -344,7 +353,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     for (int i = first; i < n_items && ok; i += stride) {
       const Item w = item_of(g, i, split);
       const int a0 = w.ta * kRows * kCG + (kCG == 2 ? (int)rank * kRows : 0) + quarter * 32, b0 = w.tb * kBN + part * kCols;
-      const int seg = kPlanes ? 1 : w.blocks;
+      const int seg = kPlanes ? 1 : kLong ? kRun : w.blocks;
       // chunks that lie in D at all
       const int chunks = a0 < g.na && b0 < g.nb ? min(kChunks, (g.nb - b0 + kC - 1) / kC) : 0;
       // the residual's next chunk is asked for a chunk ahead, a tile's first while its sums are still being formed
@@ -360,8 +369,8 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
       ask(0);
       float bias = 0.f;
       if (g.f.bias && g.f.bias_b == 0 && a0 + lane < g.na) bias = load_f32(static_cast<const T*>(g.f.bias) + (a0 + lane));
-      float acc[kPlanes ? kCols : kC];
-      if (kPlanes)
+      float acc[kKept ? kCols : kC];
+      if (kKept)
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
       for (int k = 0; k < w.blocks && ok; k += seg, ++u) {
@@ -370,7 +379,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + (u & 1u) * kBN + lanes + part * kCols;
-        if (kPlanes) {
+        if (kKept) {
 #pragma unroll
           for (int c = 0; c < kCols / 16; ++c) {
             uint32_t v[16];
@@ -406,7 +415,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(mapa(tempty + 8 * (u & 1u), kCG == 2 ? 0 : rank));
       }
-      if (kPlanes && ok) {
+      if (kKept && ok) {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
           float x[kC];
@@ -483,12 +492,12 @@ template <typename K>
 cudaError_t allow_smem(K kernel, size_t bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
-template <typename T>
+template <typename T, bool kLong>
 cudaError_t allow_all() {
-  cudaError_t e = allow_smem(k_linear_tc<T, 256, 2>, Shape<T, 256, 2>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 128, 1>, Shape<T, 128, 1>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 64, 1>, Shape<T, 64, 1>::kSmem);
-  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 32, 1>, Shape<T, 32, 1>::kSmem);
+  cudaError_t e = allow_smem(k_linear_tc<T, 256, 2, kLong>, Shape<T, 256, 2, kLong>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 128, 1, kLong>, Shape<T, 128, 1, kLong>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 64, 1, kLong>, Shape<T, 64, 1, kLong>::kSmem);
+  if (e == cudaSuccess) e = allow_smem(k_linear_tc<T, 32, 1, kLong>, Shape<T, 32, 1, kLong>::kSmem);
   return e;
 }
 template <typename K>
@@ -515,10 +524,14 @@ cudaError_t device_of(const Device** out) {
   if (!d.known) {
     if (tensor_map_encoder() == nullptr) return cudaErrorNotSupported;
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    if ((e = allow_all<float>()) != cudaSuccess || (e = allow_all<__nv_bfloat16>()) != cudaSuccess || (e = allow_all<__half>()) != cudaSuccess) return e;
-    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2>, 2, Shape<__nv_bfloat16, 256, 2>::kThreads, Shape<__nv_bfloat16, 256, 2>::kSmem);
+    if ((e = allow_all<float, false>()) != cudaSuccess || (e = allow_all<__nv_bfloat16, false>()) != cudaSuccess || (e = allow_all<__half, false>()) != cudaSuccess ||
+        (e = allow_all<__nv_bfloat16, true>()) != cudaSuccess || (e = allow_all<__half, true>()) != cudaSuccess)
+      return e;
+    using Pair = Shape<__nv_bfloat16, 256, 2, false>;
+    using One = Shape<__nv_bfloat16, 128, 1, false>;
+    d.pairs = clusters_that_fit(k_linear_tc<__nv_bfloat16, 256, 2, false>, 2, Pair::kThreads, Pair::kSmem);
     if (d.pairs < 1) return cudaErrorNotSupported;
-    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1>, n, Shape<__nv_bfloat16, 128, 1>::kThreads, Shape<__nv_bfloat16, 128, 1>::kSmem);
+    for (int n = 2; n <= 8; ++n) d.most[n] = clusters_that_fit(k_linear_tc<__nv_bfloat16, 128, 1, false>, n, One::kThreads, One::kSmem);
     d.known = true;
   }
   *out = &d;
@@ -537,21 +550,28 @@ bool encode_result(CUtensorMap* map, const Side& m, int na, int nb, int cols) {
                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int kBN, int kCG>
-cudaError_t launch(const Planes& A, const Planes& B, TcArgs g, unsigned ctas, cudaStream_t s) {
-  using S = Shape<T, kBN, kCG>;
+template <typename T, int kBN, int kCG, bool kLong>
+cudaError_t launch_kernel(const Planes& A, const Planes& B, TcArgs g, unsigned ctas, cudaStream_t s) {
+  using S = Shape<T, kBN, kCG, kLong>;
   alignas(64) CUtensorMap ma, mb, mo = {}, mr = {}, mp = {};
   if (!encode_operand(&ma, A, g.bf16, kRows) || !encode_operand(&mb, B, g.bf16, S::kCols)) return cudaErrorInvalidValue;
   constexpr int kC = S::kChunk;
   if (g.splits == 1 && !S::kNarrow) {                    // (shared tiles are finished element by element)
     g.out_tma = encode_result<T>(&mo, g.f.out, g.na, g.nb, kC);
-    g.residual_tma = !S::kPlanes && encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
+    g.residual_tma = !S::kKept && encode_result<T>(&mr, g.f.residual, g.na, g.nb, kC);
     g.preact_tma = encode_result<T>(&mp, g.f.preact, g.na, g.nb, kC);
   }
-  return launch_chained_cluster(k_linear_tc<T, kBN, kCG>, ctas, S::kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
+  return launch_chained_cluster(k_linear_tc<T, kBN, kCG, kLong>, ctas, S::kThreads, S::kSmem, s, kCG == 2 ? 2 : g.splits, ma, mb, mo, mr, mp, g);
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+template <typename T, int kBN, int kCG>
+cudaError_t launch(const Planes& A, const Planes& B, const TcArgs& g, unsigned ctas, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (ceil_div(g.blocks, g.splits) > (std::is_same<T, __half>::value ? kMostHalf : kMostBfloat)) return launch_kernel<T, kBN, kCG, true>(A, B, g, ctas, s);
+  return launch_kernel<T, kBN, kCG, false>(A, B, g, ctas, s);
+}
 
 template <typename T>
 cudaError_t launch_typed(const Device& d, const Planes& A, const Planes& B, TcArgs g, cudaStream_t s) {
