@@ -579,7 +579,7 @@ bool valid_strides(long long rs, long long cs) { return rs >= 0 && cs >= 0; }
 bool valid_in(const strads_const_matrix_t& m, int size) {
   return m.data != nullptr && ((uintptr_t)m.data % size) == 0 && valid_strides(m.row_stride, m.col_stride);
 }
-// What is written: no two elements at one place.  (Two strides with extents: the inner run must end before the outer step.)
+// What is written: no two elements at one place.  (Two strides with extents: the inner run, (n - 1) strides long, must end before the outer step.)
 bool valid_out(const strads_matrix_t& m, int size, long long rows, long long cols) {
   if (m.data == nullptr || ((uintptr_t)m.data % size) != 0 || !valid_strides(m.row_stride, m.col_stride)) return false;
   long long s1 = m.row_stride, n1 = rows, s2 = m.col_stride, n2 = cols;
@@ -587,7 +587,7 @@ bool valid_out(const strads_matrix_t& m, int size, long long rows, long long col
   if (n2 <= 1) { s2 = 0; n2 = 1; }
   if ((n1 > 1 && s1 == 0) || (n2 > 1 && s2 == 0)) return false;
   if (n1 == 1 || n2 == 1) return true;
-  return s1 <= s2 ? s2 / s1 >= n1 : s1 / s2 >= n2;
+  return s1 <= s2 ? (s2 - 1) / s1 >= n1 - 1 : (s1 - 1) / s2 >= n2 - 1;
 }
 
 int check(const strads_linear_config_t& c) {
