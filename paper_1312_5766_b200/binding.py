@@ -9,8 +9,8 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+from array import array
 
-import numpy as np
 import torch
 
 from . import workloads as wl
@@ -472,10 +472,12 @@ class AdamW:
     """AdamW over many tensors at once, moments in 32 or in 8 bits (strads_adamw_step).
 
     params are contiguous tensors of one type (float32, bfloat16, float16) on one CUDA device, stepped in place; masters,
-    with 16-bit parameters, their float32 copies, which then take the step.  moments, where given, are used as they are and
+    with 16-bit parameters, their float32 copies, which then take the step.  Where their storage is replaced (p.data = .., set_, a
+    module's .to()) the next step goes where they are then, or refuses what no longer fits.  moments, where given, are used as they are and
     kept up to date: (first, second), lists of float32 tensors, with bits=32; (codes, scales, codes, scales), lists of
     int8, float32, uint8 and float32 tensors, with bits=8 (a scale per block of 256 elements).  Otherwise they are allocated
-    here, as noughts, in the parameters' shapes.
+    here, as noughts, in the parameters' shapes.  Either way their memory is this object's from then on: `state` and `moments` give views of
+    it, and a given tensor whose storage is replaced later is no longer one.
     """
 
     def __init__(self, params, bits=32, masters=None, moments=None, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, l1=0.0):
@@ -501,30 +503,47 @@ class AdamW:
             kinds = [(torch.int8, sizes), (torch.float32, blocks), (torch.uint8, sizes), (torch.float32, blocks)]
         if moments is None:
             moments = [self._noughts(t, [p.shape for p in params] if n is sizes else [(k,) for k in n], dev) for t, n in kinds]
-        self.state = [list(m) for m in moments]
-        if len(self.state) != len(kinds):
+        self._state = [[t.detach() for t in m] for m in moments]      # views that nobody else can give another storage
+        if len(self._state) != len(kinds):
             raise ValueError(f"{len(kinds)} lists of moments expected with {bits} bits")
-        self._check("parameters", params, dtype, sizes)
-        if self.masters is not None:
-            self._check("masters", self.masters, torch.float32, sizes)
-        for m, (t, n) in zip(self.state, kinds):
-            self._check("moments", m, t, n)
-        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                         for group in (params, self.masters or [], *self.state) for t in group if t.numel())
-        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
-            raise ValueError("parameters, masters and moments must not share memory")
+        self._kinds, self._sizes, self._index = kinds, sizes, dev.index
         self._cfg = AdamWConfig(param_type=TYPES[dtype], state_bits=bits, beta1=betas[0], beta2=betas[1], eps=eps,
                                 weight_decay=weight_decay, l1=l1)
         self._list = (AdamWTensor * len(params))()
-        self._grads = np.frombuffer(self._list, dtype=np.uint64).reshape(len(params), -1)[:, AdamWTensor.grad.offset // 8]
-        self._sizes, self._index = sizes, dev.index
-        for i, p in enumerate(params):
+        words = memoryview(self._list).cast("B").cast("Q")
+        self._grads = words[AdamWTensor.grad.offset // 8::C.sizeof(AdamWTensor) // 8]
+        self._bind()
+
+    def _addresses(self):
+        """Where parameters and masters are now."""
+        at = list(map(torch.Tensor.data_ptr, self.params))
+        return at if self.masters is None else at + list(map(torch.Tensor.data_ptr, self.masters))
+
+    def _bind(self):
+        """Takes the tensors as they are now into the list that a step passes on, if they fit."""
+        self._at = None
+        self._check("parameters", self.params, self.dtype, self._sizes)
+        if self.masters is not None:
+            self._check("masters", self.masters, torch.float32, self._sizes)
+        for m, (t, n) in zip(self._state, self._kinds):
+            self._check("moments", m, t, n)
+        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                         for group in (self.params, self.masters or [], *self._state) for t in group if t.numel())
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise ValueError("parameters, masters and moments must not share memory")
+        for i, p in enumerate(self.params):
             e = self._list[i]
             e.param, e.n = p.data_ptr(), p.numel()
             e.master = self.masters[i].data_ptr() if self.masters is not None else None
-            e.m, e.v = self.state[0][i].data_ptr(), self.state[1 if bits == 32 else 2][i].data_ptr()
-            if bits == 8:
-                e.m_scale, e.v_scale = self.state[1][i].data_ptr(), self.state[3][i].data_ptr()
+            e.m, e.v = self._state[0][i].data_ptr(), self._state[1 if self.bits == 32 else 2][i].data_ptr()
+            if self.bits == 8:
+                e.m_scale, e.v_scale = self._state[1][i].data_ptr(), self._state[3][i].data_ptr()
+        self._at = self._addresses()
+
+    @property
+    def state(self):
+        """The moments as they are held: (first, second), or (codes, scales, codes, scales) of both with bits=8, lists of views."""
+        return [[t.detach() for t in m] for m in self._state]
 
     @staticmethod
     def _noughts(dtype, shapes, dev):
@@ -544,9 +563,13 @@ class AdamW:
             if t.dtype != dtype:
                 raise TypeError(f"{what} of type {t.dtype}, {dtype} expected")
 
+    def _value(self, v, dtype, default):
+        """A number, or the default and the address of one on the device."""
+        if type(v) is float or type(v) is int or not isinstance(v, torch.Tensor):      # (asking a number whether it is a tensor takes longer)
+            return v, None
+        return default, self._scalar(v, dtype)
+
     def _scalar(self, t, dtype):
-        if t is None:
-            return None
         if t.device != self.device or t.dtype != dtype or t.numel() != 1:
             raise ValueError(f"a scalar on the device must be one {dtype} on {self.device}")
         return t.data_ptr()
@@ -559,20 +582,21 @@ class AdamW:
         gtype = grads[0].dtype if grads else None
         if gtype is not torch.float32 and gtype is not self.dtype:
             raise TypeError(f"gradients of type {gtype}")
-        if ([g.numel() for g in grads] != self._sizes or {g.dtype for g in grads} != {gtype} or
-                {g.get_device() for g in grads} != {self._index} or not all([g.is_contiguous() for g in grads])):
+        if (list(map(torch.Tensor.numel, grads)) != self._sizes or {g.dtype for g in grads} != {gtype} or
+                set(map(torch.Tensor.get_device, grads)) != {self._index} or not all(map(torch.Tensor.is_contiguous, grads))):
             self._check("gradients", grads, gtype, self._sizes)
+        if self._addresses() != self._at:
+            self._bind()
         if self._index != torch._C._cuda_getDevice():
             with torch.cuda.device(self._index):
                 return self.step(grads, lr, step, grad_scale, skip)
-        c, on_device = self._cfg, lambda t: isinstance(t, torch.Tensor)
+        c = self._cfg
         c.grad_type = TYPES[gtype]
-        c.lr_dev = self._scalar(lr, torch.float32) if on_device(lr) else None
-        c.step_dev = self._scalar(step, torch.int64) if on_device(step) else None
-        c.grad_scale_dev = self._scalar(grad_scale, torch.float32) if on_device(grad_scale) else None
-        c.skip_dev = self._scalar(skip, torch.int32)
-        c.lr, c.grad_scale, c.step = 0.0 if on_device(lr) else lr, 1.0 if on_device(grad_scale) else grad_scale, 1 if on_device(step) else step
-        self._grads[:] = [g.data_ptr() for g in grads]
+        c.lr, c.lr_dev = self._value(lr, torch.float32, 0.0)
+        c.step, c.step_dev = self._value(step, torch.int64, 1)
+        c.grad_scale, c.grad_scale_dev = self._value(grad_scale, torch.float32, 1.0)
+        c.skip_dev = None if skip is None else self._scalar(skip, torch.int32)
+        self._grads[:] = array("Q", map(torch.Tensor.data_ptr, grads))
         c.stream = torch._C._cuda_getCurrentRawStream(self._index)
         rc = load().strads_adamw_step(C.byref(c), self._list, len(grads))
         if rc != OK:
@@ -582,7 +606,7 @@ class AdamW:
         """(first, second): the moments as lists of float32 tensors.  32 bits: the state itself.  8 bits: the values that the
         codes stand for, in new tensors or in `out`, a pair of lists of contiguous float32 tensors."""
         if self.bits == 32:
-            return self.state[0], self.state[1]
+            return tuple(self.state)
         sizes = [p.numel() for p in self.params]
         if out is None:
             out = [self._noughts(torch.float32, [p.shape for p in self.params], self.device) for _ in range(2)]
