@@ -373,6 +373,13 @@ def _vector(t, what, dtype, index, n):
     return t.data_ptr()
 
 
+def _refuse_autograd(where, *tensors):
+    """The layers record nothing: a result that quietly had no gradient would be lost to the program that asks for one."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise RuntimeError(f"{where} records nothing for autograd: call it under torch.no_grad(), or with detached tensors, and linear_backward for the gradient")
+
+
 def _linear_config(x, w, activation, scale, flags):
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x and w must have two dimensions")
@@ -411,7 +418,10 @@ def _linear_call(call, where, cfg, which, device):
 def linear_forward(x, w, bias=None, residual=None, activation="identity", scale=1.0, want_preact=False, out=None, preact=None, flags=0):
     """out = residual + scale * activation(x w^T + bias) (strads_linear_forward).  x [n_rows, n_in] and w [n_out, n_in] in either
     order, float32, bfloat16 or float16; residual [n_rows, n_out] may be an expanded tensor, and out may be the residual itself.
-    Returns out, and with want_preact (or preact, a tensor for it) the pair (out, x w^T + bias)."""
+    Returns out, and with want_preact (or preact, a tensor for it) the pair (out, x w^T + bias).  Nothing is recorded for autograd (linear_backward is the
+    gradient): while that is on, tensors that require a gradient are refused."""
+    if torch.is_grad_enabled():
+        _refuse_autograd("linear_forward", x, w, bias, residual, out, preact)
     cfg, n, _, m, dtype, index = _linear_config(x, w, activation, scale, flags)
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
@@ -437,7 +447,9 @@ def linear_backward(grad_out, x, w, preact=None, activation="identity", scale=1.
                     grad_x=None, grad_w=None, grad_bias=None, flags=0):
     """Gradients of linear_forward (strads_linear_backward) from grad_out [n_rows, n_out] and the preact that the forward pass gave
     (not with the identity): (grad_x, grad_w, grad_bias), None where not wanted.  New gradients have the order of x and w.  The residual's
-    gradient is grad_out itself."""
+    gradient is grad_out itself.  Not differentiable itself: as in linear_forward, tensors that require a gradient are refused while autograd is on."""
+    if torch.is_grad_enabled():
+        _refuse_autograd("linear_backward", grad_out, x, w, preact, grad_x, grad_w, grad_bias)
     cfg, n, k, m, dtype, index = _linear_config(x, w, activation, scale, flags)
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
