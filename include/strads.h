@@ -418,7 +418,7 @@ typedef struct {
 typedef struct {
   int32_t param_type, grad_type;        /* strads_type_t                                          */
   int32_t state_bits;                   /* 32 or 8                                                */
-  double  lr, beta1, beta2, eps;        /* lr >= 0, 0 <= beta < 1, eps > 0                        */
+  double  lr, beta1, beta2, eps;        /* lr >= 0, 0 <= beta < 1, eps >= 2^-126                  */
   double  weight_decay, l1;             /* >= 0                                                   */
   double  grad_scale;
   int64_t step;                         /* t >= 1 (ignored with step_dev)                         */

@@ -411,6 +411,7 @@ int by_grad(int grad_type, bool master, int bits, const Entry* list, int count, 
 }
 
 constexpr long long kMaxElements = 1ll << 40;
+constexpr float kLeastEps = 1.17549435e-38f;      // 2^-126: a smaller one's inverse may be infinite, and 0 times that (both moments 0) no step
 
 // No two tensors may share parameters: the order in which they would be written is open.  Lists in the order of their
 // addresses, as views of one flat buffer are, are checked on the way through.
@@ -451,7 +452,7 @@ int strads_adamw_step(const strads_adamw_config_t* cfg, const strads_adamw_tenso
   if (c.param_type < STRADS_F32 || c.param_type > STRADS_F16) return STRADS_ERR_INVALID_ARG;
   if (c.grad_type != STRADS_F32 && c.grad_type != c.param_type) return STRADS_ERR_INVALID_ARG;
   if (!(c.lr >= 0.0 && c.lr <= 1e30) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
-      !((float)c.eps > 0.f && c.eps <= 1e30) || !(c.weight_decay >= 0.0 && c.weight_decay <= 1e30) || !(c.l1 >= 0.0 && c.l1 <= 1e30) ||
+      !((float)c.eps >= kLeastEps && c.eps <= 1e30) || !(c.weight_decay >= 0.0 && c.weight_decay <= 1e30) || !(c.l1 >= 0.0 && c.l1 <= 1e30) ||
       !(std::fabs(c.grad_scale) <= 1e30) || (c.step < 1 && c.step_dev == nullptr))
     return STRADS_ERR_INVALID_ARG;
   const size_t ps = size_of(c.param_type), gs = size_of(c.grad_type), ss = c.state_bits == 32 ? 4 : 1;
