@@ -321,7 +321,7 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  *
  * All arrays of a call have one type (strads_type_t).  Sums are held in 32 bits or more; where additions truncate (16-bit products), no more terms
  * go into one accumulator than cost a tenth of the result's rounding.  binary32 products go through three
- * bfloat16 parts of each operand (24 bits together) on the tensor cores, or are formed as they are where one side has few
+ * bfloat16 parts of each operand (24 bits together; below 2^-110, what lies above 2^-134) on the tensor cores, or are formed as they are where one side has few
  * rows; an infinity among binary32 operands may come out as NaN.  16-bit types: through an activation gz (without scale) is rounded
  * where the products read it, an error as large as the result's own rounding: gx and gw are about sqrt(2) further from the formula than with gz in
  * 32 bits; gbias is not.  bfloat16's gz is rounded to the type; binary16's to its 11 bits with a power of two of its row (for gx) or column (for gw), so
@@ -331,14 +331,14 @@ int strads_sample_static(const float* delta_dev, int64_t n_cols, float eta, uint
  * -infinity NaN, the formula's -infinity times 0.  Slopes at the infinities are their limits (a 16-bit z past the type's range is kept as one).
  *
  * Matrices may have any strides (elements; >= 0 for what is read, so rows and columns may be repeated with stride 0; what is
- * written must not overlap itself or any input, but out may be the residual itself).  Best are operands with one stride of 1,
+ * written must not overlap itself, another result or any input, but out may be the residual itself).  Best are operands with one stride of 1,
  * the other a multiple of 16 bytes and 16-byte aligned data, either order: these are read in place.  Others are first copied
  * into the workspace, as are binary32 operands.
  *
  * The workspace (device, 256-byte aligned) holds nothing between calls; two calls that may run at the same time need one each.
  * No allocation, no host synchronisation; may be captured.  Asynchronous on `stream`, on the current device, which must hold
  * all arrays.  Same inputs, same bits.
- * Should a bounded wait run out (see strads_set_wait_limit), the outputs are undefined and strads_linear_status says so:
+ * Should a bounded wait run out (each gives up after a fixed number of polls, which amounts to seconds), the outputs are undefined and strads_linear_status says so:
  * it waits for the device, and returns STRADS_OK or STRADS_ERR_TIMEOUT and the bits raised on the current device since the last
  * call of it.  STRADS_LINEAR_FLAG_STALL withholds a call's operand loads, so that its waits run out after milliseconds. */
 typedef enum { STRADS_F32 = 0, STRADS_BF16 = 1, STRADS_F16 = 2 } strads_type_t;

@@ -58,3 +58,17 @@ def test_slopes_at_the_ends(b, act, dtype, n):
         good = ~row.isnan()
         gx, _, _ = b.linear_backward(one[:, good], torch.ones(n, 16, dtype=dtype, device="cuda"), torch.eye(int(good.sum()), 16, dtype=dtype, device="cuda"), preact=z[:, good], activation=act)
         same(gx, want[:, good][:, :16], dtype)
+
+
+@pytest.mark.parametrize("n,m", [(3, 100), (20, 1000), (200, 300)])
+@pytest.mark.parametrize("power", [-100, -111, -118, -124])
+def test_small_binary32_operands(b, n, m, power):
+    """Three parts of 8 bits hold what lies above 2^-134 (half the smallest bfloat16) of an operand: the usual bound and that much of every x more."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    k = 500
+    x, w = torch.randn(n, k, generator=gen, device="cuda") * 2.0 ** power, torch.randn(m, k, generator=gen, device="cuda") * 2.0 ** 100
+    want, s = x.to(F64) @ w.to(F64).t(), x.to(F64).abs() @ w.to(F64).abs().t()
+    got = b.linear_forward(x, w).to(F64)
+    assert ((got - want).abs() <= (k + 16) * 2.0 ** -24 * s + 2.0 ** -134 * w.to(F64).abs().sum(1)).all()
+    _, gw, _ = b.linear_backward(w.t(), x.t(), x.new_empty(m, n), want_x=False, want_bias=False)
+    assert ((gw.to(F64) - want.t()).abs() <= (k + 16) * 2.0 ** -24 * s.t() + 2.0 ** -134 * w.to(F64).abs().sum(1)[:, None]).all()
