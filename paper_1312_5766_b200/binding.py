@@ -373,15 +373,14 @@ def _vector(t, what, dtype, index, n):
     return t.data_ptr()
 
 
-def _refuse_autograd(where, *tensors):
+def _refuse_autograd(where):
     """The layers record nothing: a result that quietly had no gradient would be lost to the program that asks for one."""
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            raise RuntimeError(f"{where} records nothing for autograd: call it under torch.no_grad(), or with detached tensors, and linear_backward for the gradient")
+    raise RuntimeError(f"{where} records nothing for autograd: call it under torch.no_grad(), or with detached tensors, and linear_backward for the gradient")
 
 
 def _linear_config(x, w, activation, scale, flags):
-    if x.dim() != 2 or w.dim() != 2:
+    xs, ws = x.shape, w.shape
+    if len(xs) != 2 or len(ws) != 2:
         raise ValueError("x and w must have two dimensions")
     index, dtype = x.get_device(), x.dtype
     if index < 0:
@@ -390,9 +389,9 @@ def _linear_config(x, w, activation, scale, flags):
         raise TypeError(f"x of type {dtype}")
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
-    n, k = x.shape
-    m = w.shape[0]
-    if w.dtype != dtype or w.get_device() != index or w.shape[1] != k:
+    n, k = xs
+    m = ws[0]
+    if w.dtype != dtype or w.get_device() != index or ws[1] != k:
         _refuse(w, "w", dtype, index, (m, k))
     xr, xc = x.stride()
     wr, wc = w.stride()
@@ -420,8 +419,10 @@ def linear_forward(x, w, bias=None, residual=None, activation="identity", scale=
     order, float32, bfloat16 or float16; residual [n_rows, n_out] may be an expanded tensor, and out may be the residual itself.
     Returns out, and with want_preact (or preact, a tensor for it) the pair (out, x w^T + bias).  Nothing is recorded for autograd (linear_backward is the
     gradient): while that is on, tensors that require a gradient are refused."""
-    if torch.is_grad_enabled():
-        _refuse_autograd("linear_forward", x, w, bias, residual, out, preact)
+    if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad) or
+                                    (residual is not None and residual.requires_grad) or (out is not None and out.requires_grad) or
+                                    (preact is not None and preact.requires_grad)):
+        _refuse_autograd("linear_forward")
     cfg, n, _, m, dtype, index = _linear_config(x, w, activation, scale, flags)
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
@@ -448,8 +449,10 @@ def linear_backward(grad_out, x, w, preact=None, activation="identity", scale=1.
     """Gradients of linear_forward (strads_linear_backward) from grad_out [n_rows, n_out] and the preact that the forward pass gave
     (not with the identity): (grad_x, grad_w, grad_bias), None where not wanted.  New gradients have the order of x and w.  The residual's
     gradient is grad_out itself.  Not differentiable itself: as in linear_forward, tensors that require a gradient are refused while autograd is on."""
-    if torch.is_grad_enabled():
-        _refuse_autograd("linear_backward", grad_out, x, w, preact, grad_x, grad_w, grad_bias)
+    if torch.is_grad_enabled() and (grad_out.requires_grad or x.requires_grad or w.requires_grad or (preact is not None and preact.requires_grad) or
+                                    (grad_x is not None and grad_x.requires_grad) or (grad_w is not None and grad_w.requires_grad) or
+                                    (grad_bias is not None and grad_bias.requires_grad)):
+        _refuse_autograd("linear_backward")
     cfg, n, k, m, dtype, index = _linear_config(x, w, activation, scale, flags)
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):

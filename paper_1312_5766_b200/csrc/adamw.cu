@@ -308,8 +308,8 @@ __device__ __forceinline__ void step_block(const Entry& e, const Scalars& c, lon
   }
 }
 
-// 8 bits: five CTAs to an SM (48 registers): bound by issuing some 85 instructions an element, it wants the warps (341 -> 320 us at 100 M
-// parameters; six CTAs, with spills, 352).
+// 8 bits: five CTAs to an SM (48 registers, 4 to 8 bytes spilled, and a frame of 80 for the rare exact roots): bound by issuing some 85 instructions an
+// element, it wants the warps (341 -> 320 us at 100 M parameters; six CTAs, with more spills, 352).
 template <typename P, typename G, bool kMaster, int kBits, int kCap>
 __global__ void __launch_bounds__(kThreads, kBits == 8 ? 5 : 1) k_adamw(const __grid_constant__ Table<kCap> t, const __grid_constant__ Step s) {
   if (s.skip_dev != nullptr && *s.skip_dev != 0) return;

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads) k_linear_tops(Operand gout, long lon
 // A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row, kU of them at a time so that their loads are under way
 // together.  Three CTAs to an SM (80 registers): the pass waits for memory, and warps hide that better than rows of one lane (gradient of 4,096 x 8,192
 // bfloat16 by 64, SiLU / GELU: 62 / 69 us; four rows at a time and one CTA 99 / 80, two CTAs 66 / 75; four CTAs 60 / 66, with spills that cost binary32
-// and small ones more).  gz (may be null) [n][ld], rounded to T; partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
+// and small ones more; at three, instances spill up to 72 bytes, binary16's with lines up to 296, which one row at a time avoids but takes longer: 119 -> 124).  gz (may be null) [n][ld], rounded to T; partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
 template <typename T, bool kVec>
 __device__ __forceinline__ void load8(const T* p, long long stride, int count, T (&x)[8]) {
   if (kVec) {
@@ -187,7 +187,7 @@ __device__ __forceinline__ void gz_rows(const Operand& gout, const Operand& prea
   constexpr bool kLines = std::is_same<T, __half>::value && kAct != STRADS_ACT_IDENTITY;
   constexpr int kU = 2;
   const int count = (int)min(8ll, m - c);
-  float power[kLines ? 8 : 1];
+  float power[kLines ? 8 : 1] = {};
   if (kLines && lines.by_column != nullptr)
 #pragma unroll
     for (int j = 0; j < (kLines ? 8 : 0); ++j) power[j] = line_power(lines.column_factors[c + min(j, count - 1)]);
@@ -386,11 +386,16 @@ Product plan(Call& c, Matrix& A, bool ta, Matrix& B, bool tb, const Finish& f) {
   const bool unknown = (d.b_long ? B : A).unknown;       // (a query: room for any way)
   // Few rows on one side: streamed, if the tensor cores would first have to copy the long side or split it; 16-bit ones that they read where they are go
   // there at once (4,096 x 4,096 bfloat16: 11 us whatever the rows, streamed 14 with two, 13 with four), but for one row with k along memory (10.7) and
-  // for long sides of so few rows that they make few tiles (64 rows of 16,384: 13.6, streamed 3.8).
+  // for long sides of so few rows that they make few tiles.  Those, four rows, out of cold L2, streamed / tensor cores: k along memory, 16,384 of it, 64 rows of
+  // the long side 10 / 20 us, 512 14 / 23, 1,024 23 / 25, 1,536 31 / 27, 2,048 37 / 29; k = 1,024: 8 / 12, 8 / 12, 10 / 12, 12 / 12, 14 / 14.  (Rows along memory and
+  // k = 16,384 the tensor cores are ahead throughout, 39 / 21 at 64 rows; k = 1,024 level.)
+  // binary32, streamed / split: 4,096 x 4,096, one row 23 / 31, four 31 / 31; 1,000 x 10,000 21 / 29, 23 / 29; 10,000 x 20,000 by columns 141 / 156, 170 / 158, by rows
+  // 162 / 152, 301 / 150.
   d.way = Product::kThin;
   if (ns <= kThinMost && !unknown && (c.size == 4 || !in_place(l, nl, d.nk) || (ns == 1 && l.ks == 1) || nl < 2048)) return d;
   // binary32 with up to kSplitMost rows on one side: the other is read once, where it is, and split on the way (4 bytes an element for every 32 or 48
-  // rows, most of them from L2, where planes in memory cost 16)
+  // rows, most of them from L2, where planes in memory cost 16).  Split / planes: 10,000 x 20,000 by 8 rows 150 / 643 us, by 128 395 / 864, by 256 760 / 1,333; 4,096 x
+  // 4,096 31 / 84, 49 / 78, 82 / 98: the planes' own rule would be later still.
   if (c.size == 4 && ns <= kSplitMost && (unknown || linear_split_takes(l, nl, d.nk))) {
     d.way = Product::kSplit;
     d.pb = bring(c, sh, ns, d.nk, false, true);

@@ -32,7 +32,8 @@ __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void store_f32(__half* p, float v) { *p = __float2half_rn(v); }
 
-// For binary32 results (kExact) CUDA's exponential and quotient, for 16-bit ones the hardware's, good to 2^-20.  Phi(-z), z >= 0, is exp(-z^2/2)
+// For binary32 results (kExact) CUDA's exponential and quotient, for 16-bit ones the hardware's, good to 2^-20 for
+// arguments up to 16 and, by the rounding of x log2(e), to 2^-18 at 80 (16-bit results are rounded by 2^-12 at least).  Phi(-z), z >= 0, is exp(-z^2/2)
 // t P(t), t = 1 / (1 + 0.285 z): P is fitted to erfcx, weighted so that the relative error is even (1.6e-7; 4.7e-7 as evaluated here).  Nothing
 // cancels for negative z in any of them.
 __device__ __forceinline__ float fast_inverse(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }

@@ -2,7 +2,7 @@
 // reading the long side once, so it is read where it is, 4 bytes an element, and split into three bfloat16 planes on its way into
 // tensor memory; the short side comes as planes in memory (written by the pass before).
 //
-// A tile is 128 rows of the long side by kBN = 32 or 48 of the short one.  One thread brings blocks of 64 k by TMA, the long side's as it is (the
+// A tile is 128 rows of the long side by kBN = 32 or 48 of the short one (48: 128 registers and 188 bytes spilled).  One thread brings blocks of 64 k by TMA, the long side's as it is (the
 // ring holds 160 KB of it: what hides the memory's latency); eight warps, a lane per row, split them and put the planes into tensor
 // memory, which the tensor cores take their A operand from: shared memory, whose bandwidth would otherwise bound the kernel, is written and
 // read once for every element.  One thread issues the products.  The short side's planes lie one behind the other as rows of B, so three

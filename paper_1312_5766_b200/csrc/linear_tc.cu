@@ -483,7 +483,7 @@ k_linear_tc(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 }
 
 // What is asked of the driver once per process and device.
-struct Device { bool known; int sms; int pairs; int most[9]; };      // most[n]: clusters of n CTAs that fit at once
+struct Device { bool known; int sms; int pairs; int most[9]; };      // most[n]: clusters of n CTAs that fit at once (of bfloat16's 128 columns; every 128-column kernel has an SM to itself)
 constexpr int kMaxDevices = 64;
 std::mutex g_mutex;
 Device g_device[kMaxDevices];
