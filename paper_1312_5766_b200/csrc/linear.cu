@@ -170,7 +170,8 @@ __global__ void __launch_bounds__(kThreads) k_linear_tops(Operand gout, long lon
 // A CTA takes 256 columns of `rows` rows, a lane eight columns, a warp every eighth row, kU of them at a time so that their loads are under way
 // together.  Three CTAs to an SM (80 registers): the pass waits for memory, and warps hide that better than rows of one lane (gradient of 4,096 x 8,192
 // bfloat16 by 64, SiLU / GELU: 62 / 69 us; four rows at a time and one CTA 99 / 80, two CTAs 66 / 75; four CTAs 60 / 66, with spills that cost binary32
-// and small ones more; at three, instances spill up to 72 bytes, binary16's with lines up to 296, which one row at a time avoids but takes longer: 119 -> 124).  gz (may be null) [n][ld], rounded to T; partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
+// and small ones more; at three, instances spill up to 72 bytes, binary16's with lines up to 296, which one row at a time avoids but takes longer: 119 -> 124).
+// gz (may be null) [n][ld], rounded to T; partial (may be null) [gridDim.y][m]: the sums of the CTA's rows, of gz before its rounding.
 template <typename T, bool kVec>
 __device__ __forceinline__ void load8(const T* p, long long stride, int count, T (&x)[8]) {
   if (kVec) {
@@ -466,7 +467,7 @@ Gz<T> plan_z(Call& c, const strads_linear_config_t& g, bool want_x, bool want_w,
   k.ld = (g.n_out + 7) / 8 * 8;
   const size_t n = (size_t)g.n_rows, m = (size_t)g.n_out, bytes = n * (size_t)k.ld * sizeof(T);
   if (k.formed && (want_x || !k.by_lines)) k.for_x = static_cast<T*>(c.take(bytes));
-  k.for_w = k.by_lines && want_w ? static_cast<T*>(c.take(bytes)) : k.for_x;
+  k.for_w = !k.by_lines ? k.for_x : want_w ? static_cast<T*>(c.take(bytes)) : nullptr;
   if (k.by_lines && want_x) {
     k.row_tops = static_cast<unsigned short*>(c.take(n * (size_t)k.columns * 2));
     k.row_factors = static_cast<float*>(c.take(n * 4));

@@ -112,3 +112,17 @@ def test_every_share_of_rows_and_columns(b, n, m):
     gout = (torch.randn(n, m, generator=gen, device="cuda") * rows[:, None] * cols).half()
     z, x, w = (matrix(*s, torch.float16, gen, scale=f) for s, f in (((n, m), 1.0), ((n, k), 1e-3), ((m, k), 1e-3)))
     check_gradient(b, gout, x, w, z, "silu", 0.5, of_the_largest)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ["identity", "relu", "gelu"])
+@pytest.mark.parametrize("n,k,m", [(15, 14, 9), (3, 300, 500), (300, 1, 40), (700, 130, 260)])
+def test_every_choice_of_gradients(b, n, k, m, act, dtype):
+    """Each of gx, gw and gbias with and without the others: the same bits."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    gout, z, x, w = (matrix(*s, dtype, gen) for s in ((n, m), (n, m), (n, k), (m, k)))
+    every = b.linear_backward(gout, x, w, preact=z, activation=act, scale=0.5)
+    for want in range(1, 8):
+        got = b.linear_backward(gout, x, w, preact=z, activation=act, scale=0.5, want_x=bool(want & 1), want_w=bool(want & 2), want_bias=bool(want & 4))
+        for i in range(3):
+            assert torch.equal(got[i], every[i]) if want >> i & 1 else got[i] is None
